@@ -1,0 +1,96 @@
+/*
+ * libframequant, losses over the vocabulary: what quantization costs a model (its perplexity)
+ * and how the loss is won back (distillation from the unquantized model), computed from the
+ * last hidden states x and the output weight W without keeping the logits s = x W^T.
+ *
+ * For token t with hidden state x_t (row of x, M x d) and vocabulary entry v (row of W, V x d):
+ *
+ *   cross entropy   lse_t = log sum_v exp(s_tv),   loss_t = lse_t - s_{t, target_t}
+ *                   ds_tv = dloss_t (exp(s_tv - lse_t) - [v = target_t])
+ *
+ *   distillation    z = s / tau,  lse_t = log sum_v exp(z_tv),
+ *                   p_tk = softmax over token t's entries k of logit_tk / tau
+ *                   loss_t = tau^2 sum_k p_tk (log p_tk - z_{t, index_tk} + lse_t)
+ *                   ds_tv = dloss_t tau (exp(z_tv - lse_t) - sum_k p_tk [index_tk = v])
+ *
+ *   both            dx = ds W (M x d),  dW = ds^T x (V x d)
+ *
+ * The logits live in tensor memory, one tile at a time.  The gradient calls recompute them and
+ * hold ds, rounded to bf16, one piece of the vocabulary at a time in the workspace (at most
+ * 128 MiB, or 2048 vocabulary entries where M is so large that these take more).
+ *
+ * A token without a target (target_t < 0; no entry with index_tk >= 0 and logit_tk > -inf)
+ * has loss 0 and lse 0 and contributes nothing to a gradient, whatever its hidden state and its
+ * dloss hold (infinities and NaN included).  Entries of one token may come in any order; equal
+ * indices add up.  A target or index >= V is reported as FQ_ERR_DEVICE_CHECK in the workspace's
+ * status word (fq_check) and counts as none.
+ *
+ * Conventions are those of framequant.h (device pointers, 16-byte alignment, asynchronous on
+ * `stream`, validation before any launch, no allocation by the library).  The workspace need
+ * not be cleared.  x, W, dx and dW are bf16, row-major; sums and softmax statistics are fp32.
+ * Results do not depend on the order in which blocks run: a call repeated on the same inputs
+ * gives the same bits.
+ */
+#ifndef FRAMEQUANT_HEAD_H_
+#define FRAMEQUANT_HEAD_H_
+
+#include "framequant.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Largest number of teacher entries per token. */
+#define FQ_DISTILL_MAX_K 1024
+
+/* Workspace bytes of fq_cross_entropy (K = 1) and fq_distill for M tokens; 0 for invalid sizes
+ * (M, d, V < 1, K outside [1, FQ_DISTILL_MAX_K]). */
+size_t fq_head_workspace_bytes(int M, int d, int V, int K);
+
+/* Workspace bytes of fq_cross_entropy_grad (K = 1) and fq_distill_grad; 0 for invalid sizes. */
+size_t fq_head_grad_workspace_bytes(int M, int d, int V, int K);
+
+/* Cross entropy of M tokens.
+ *   x       device bf16 M x d;  W  device bf16 V x d;  target  device int32 M
+ *   loss    device fp32 M output;  lse  device fp32 M output (the gradient call takes it)
+ *   ws      device workspace of fq_head_workspace_bytes(M, d, V, 1) bytes, 256-byte aligned
+ * Requirements: M, d, V >= 1, d a multiple of 8.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_ALIGNMENT, FQ_ERR_WORKSPACE, FQ_ERR_UNSUPPORTED (device
+ * not compute capability 10.3), FQ_ERR_CUDA. */
+fq_status fq_cross_entropy(const void* x, int M, int d, const void* W, int V,
+                           const int32_t* target, float* loss, float* lse, void* ws,
+                           size_t ws_bytes, fq_stream_t stream);
+
+/* Gradient of sum_t dloss_t loss_t.
+ *   lse    as written by fq_cross_entropy for the same x, W and target
+ *   dloss  device fp32 M
+ *   dx     device bf16 M x d output, or NULL;  dW  device bf16 V x d output, or NULL (a frozen
+ *          output weight); at least one of them
+ *   ws     device workspace of fq_head_grad_workspace_bytes(M, d, V, 1) bytes
+ * Requirements and errors as fq_cross_entropy. */
+fq_status fq_cross_entropy_grad(const void* x, int M, int d, const void* W, int V,
+                                const int32_t* target, const float* lse, const float* dloss,
+                                void* dx, void* dW, void* ws, size_t ws_bytes,
+                                fq_stream_t stream);
+
+/* Distillation loss of M tokens from the teacher's K largest logits.
+ *   index  device int32 M x K (vocabulary entries; < 0: no entry)
+ *   logit  device fp32 M x K (the teacher's logits of those entries)
+ *   tau    temperature, finite and > 0
+ * Other arguments, requirements and errors as fq_cross_entropy; 1 <= K <= FQ_DISTILL_MAX_K. */
+fq_status fq_distill(const void* x, int M, int d, const void* W, int V, const int32_t* index,
+                     const float* logit, int K, float tau, float* loss, float* lse, void* ws,
+                     size_t ws_bytes, fq_stream_t stream);
+
+/* Gradient of sum_t dloss_t loss_t with respect to the student's x and W, arguments as in
+ * fq_distill and fq_cross_entropy_grad. */
+fq_status fq_distill_grad(const void* x, int M, int d, const void* W, int V,
+                          const int32_t* index, const float* logit, int K, float tau,
+                          const float* lse, const float* dloss, void* dx, void* dW, void* ws,
+                          size_t ws_bytes, fq_stream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* FRAMEQUANT_HEAD_H_ */

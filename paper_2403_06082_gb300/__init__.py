@@ -26,9 +26,12 @@ __all__ = [
     "fq_linear_forward_group", "Layer", "FQ_MAX_GROUP", "fq_gptq_hessian",
     "fq_gptq_workspace_bytes", "fq_quantize_gptq", "fq_implicit_group_workspace_bytes",
     "fq_linear_forward_implicit_group", "ImplicitLayer", "fq_frame_tiles_bytes", "fq_frame_tile",
+    "fq_head_workspace_bytes", "fq_head_grad_workspace_bytes", "fq_cross_entropy",
+    "fq_cross_entropy_grad", "fq_distill", "fq_distill_grad", "FQ_DISTILL_MAX_K",
 ]
 FQ_MAX_GROUP = 4
 FQ_STATIC_SCRATCH_BYTES = 16 << 20
+FQ_DISTILL_MAX_K = 1024
 
 FQ_BF16 = 0
 FQ_FP32_DEBUG = 1
@@ -51,7 +54,9 @@ EXPORTED = ("fq_packed_words", "fq_pack", "fq_workspace_bytes", "fq_linear_forwa
             "fq_dense_forward", "fq_static_check", "fq_group_workspace_bytes",
             "fq_linear_forward_group", "fq_gptq_hessian", "fq_gptq_workspace_bytes",
             "fq_quantize_gptq", "fq_implicit_group_workspace_bytes",
-            "fq_linear_forward_implicit_group", "fq_frame_tiles_bytes", "fq_frame_tile")
+            "fq_linear_forward_implicit_group", "fq_frame_tiles_bytes", "fq_frame_tile",
+            "fq_head_workspace_bytes", "fq_head_grad_workspace_bytes", "fq_cross_entropy",
+            "fq_cross_entropy_grad", "fq_distill", "fq_distill_grad")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -224,6 +229,20 @@ def lib() -> ctypes.CDLL:
         L.fq_quantize_rtn.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                       ctypes.c_void_p, ctypes.c_void_p]
+        vp, ci, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+        for name in ("fq_head_workspace_bytes", "fq_head_grad_workspace_bytes"):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [ci] * 4
+        L.fq_cross_entropy.restype = ci
+        L.fq_cross_entropy.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, vp, sz, vp]
+        L.fq_cross_entropy_grad.restype = ci
+        L.fq_cross_entropy_grad.argtypes = [vp, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.fq_distill.restype = ci
+        L.fq_distill.argtypes = [vp, ci, ci, vp, ci, vp, vp, ci, ctypes.c_float, vp, vp, vp, sz,
+                                 vp]
+        L.fq_distill_grad.restype = ci
+        L.fq_distill_grad.argtypes = [vp, ci, ci, vp, ci, vp, vp, ci, ctypes.c_float, vp, vp, vp,
+                                      vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -583,3 +602,67 @@ def fq_quantize_rtn(C, n_out: int, n_in: int, codes, scale, zero, gamma=None,
                     stream=None) -> None:
     _ok(lib().fq_quantize_rtn(_ptr(C), n_out, n_in, _ptr(codes), _ptr(scale), _ptr(zero),
                               _ptr(gamma), _stream(stream)), "fq_quantize_rtn")
+
+
+# ------------------------------------------------------------------ losses over the vocabulary
+def _arr(t, dtype: str, count: int, what: str):
+    """_ptr of a tensor that has to hold at least `count` values of the named torch dtype (None
+    passes through); what the C side cannot see is refused here."""
+    if t is None:
+        return None
+    if str(t.dtype) != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if t.numel() < count:
+        raise ValueError(f"{what}: {count} values expected, got {t.numel()}")
+    return _ptr(t)
+
+
+_BF, _F32, _I32 = "torch.bfloat16", "torch.float32", "torch.int32"
+
+
+def fq_head_workspace_bytes(M: int, d: int, V: int, K: int = 1) -> int:
+    return lib().fq_head_workspace_bytes(M, d, V, K)
+
+
+def fq_head_grad_workspace_bytes(M: int, d: int, V: int, K: int = 1) -> int:
+    return lib().fq_head_grad_workspace_bytes(M, d, V, K)
+
+
+def fq_cross_entropy(x, M: int, d: int, W, V: int, target, loss, lse, ws, ws_bytes: int,
+                     stream=None) -> None:
+    """Cross entropy of M tokens from their last hidden states x and the output weight W,
+    without keeping the logits (include/framequant_head.h); target < 0: no target."""
+    _ok(lib().fq_cross_entropy(_arr(x, _BF, M * d, "x"), M, d, _arr(W, _BF, V * d, "W"), V,
+                               _arr(target, _I32, M, "target"), _arr(loss, _F32, M, "loss"),
+                               _arr(lse, _F32, M, "lse"), _ptr(ws), ws_bytes, _stream(stream)),
+        "fq_cross_entropy")
+
+
+def fq_cross_entropy_grad(x, M: int, d: int, W, V: int, target, lse, dloss, dx, dW, ws,
+                          ws_bytes: int, stream=None) -> None:
+    """Gradient of sum_t dloss_t loss_t into dx and dW (either may be None)."""
+    _ok(lib().fq_cross_entropy_grad(
+        _arr(x, _BF, M * d, "x"), M, d, _arr(W, _BF, V * d, "W"), V,
+        _arr(target, _I32, M, "target"), _arr(lse, _F32, M, "lse"),
+        _arr(dloss, _F32, M, "dloss"), _arr(dx, _BF, M * d, "dx"), _arr(dW, _BF, V * d, "dW"),
+        _ptr(ws), ws_bytes, _stream(stream)), "fq_cross_entropy_grad")
+
+
+def fq_distill(x, M: int, d: int, W, V: int, index, logit, K: int, tau: float, loss, lse, ws,
+               ws_bytes: int, stream=None) -> None:
+    """Distillation loss of M tokens from the teacher's K largest logits (index, logit: M x K;
+    index < 0: no entry) at temperature tau (include/framequant_head.h)."""
+    _ok(lib().fq_distill(_arr(x, _BF, M * d, "x"), M, d, _arr(W, _BF, V * d, "W"), V,
+                         _arr(index, _I32, M * K, "index"), _arr(logit, _F32, M * K, "logit"), K,
+                         tau, _arr(loss, _F32, M, "loss"), _arr(lse, _F32, M, "lse"), _ptr(ws),
+                         ws_bytes, _stream(stream)), "fq_distill")
+
+
+def fq_distill_grad(x, M: int, d: int, W, V: int, index, logit, K: int, tau: float, lse, dloss,
+                    dx, dW, ws, ws_bytes: int, stream=None) -> None:
+    """Gradient of sum_t dloss_t loss_t into dx and dW (either may be None)."""
+    _ok(lib().fq_distill_grad(
+        _arr(x, _BF, M * d, "x"), M, d, _arr(W, _BF, V * d, "W"), V,
+        _arr(index, _I32, M * K, "index"), _arr(logit, _F32, M * K, "logit"), K, tau,
+        _arr(lse, _F32, M, "lse"), _arr(dloss, _F32, M, "dloss"), _arr(dx, _BF, M * d, "dx"),
+        _arr(dW, _BF, V * d, "dW"), _ptr(ws), ws_bytes, _stream(stream)), "fq_distill_grad")

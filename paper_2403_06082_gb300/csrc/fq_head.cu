@@ -1,0 +1,958 @@
+// Losses over the vocabulary and their gradients (include/framequant_head.h) on the sm_103a
+// tensor cores, without keeping the logits.
+//
+// One persistent, warp-specialised kernel computes tiles of  acc[i][j] = sum_k A[i][k] B[j][k]
+// (128 rows of A on the tensor core's rows, bn <= 256 rows of B on its columns, fp32 in TMEM)
+// for the four products of a training step:
+//   kLse  A = x (tokens),   B = W (vocabulary),  k = d: per token and tile the running maximum
+//         and sum of exponentials, and the logits of the token's targets;
+//   kDl   the same product again: ds = g (softmax - target) as bf16, one piece of the vocabulary;
+//   kDx   A = ds (tokens),  B = W^T (d columns), k = the piece: dx;
+//   kDw   A = ds^T (vocabulary rows), B = x^T (d columns), k = tokens: dW of the piece.
+// A token is a row of the accumulator, i.e. one epilogue thread, so the softmax statistics of a
+// tile need no exchange between threads.  Operands whose contraction dimension is not the
+// contiguous one (W in kDx, ds and x in kDw) are read as they lie in memory, as MN-major tiles:
+// nothing is transposed.
+//
+// Warp roles: warp 0 TMA producer (one lane), warp 1 TMEM owner + MMA issuer (one lane),
+// warps 2-5 epilogue (thread = accumulator row).
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <math_constants.h>
+
+#include <algorithm>
+#include <cmath>
+#include <map>
+#include <mutex>
+
+#include "fq_device.cuh"
+#include "fq_internal.h"
+#include "framequant_head.h"
+
+namespace fq {
+namespace {
+
+enum Mode : int { kLse = 0, kDl = 1, kDx = 2, kDw = 3 };
+
+constexpr int kBM = 128;                        // accumulator rows per tile
+constexpr int kBN = 256;                        // accumulator columns per tile, at most
+constexpr int kBK = 64;                         // k per stage: one 128-byte swizzle row of bf16
+constexpr int kABytes = kBM * kBK * 2;
+constexpr int kBBytes = kBN * kBK * 2;
+constexpr int kAtomBytes = 64 * kBK * 2;        // MN-major: 64 rows of the operand x kBK
+constexpr int kStages = 4;
+constexpr int kThreads = 192;
+constexpr int kEpi = 128;
+constexpr int kChunk = 32;                      // accumulator columns per epilogue step
+constexpr int kTmemCols = 2 * kBN;
+constexpr int kNone = 0x7fffffff;               // sorted entry lists: no entry
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+constexpr int oA = 0;
+constexpr int oB = oA + kStages * kABytes;
+constexpr int oBar = oB + kStages * kBBytes;
+constexpr int oMisc = oBar + (2 * kStages + 5) * 8;
+constexpr int kSmemBytes = oMisc + 16 + 1024;   // + alignment slack
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+
+constexpr bool a_mn_major(int mode) { return mode == kDw; }
+constexpr bool b_mn_major(int mode) { return mode == kDx || mode == kDw; }
+
+struct GemmArgs {
+  int R, N, K;                // rows of A, rows of B (columns of the result), contraction
+  int bn;                     // columns per tile (multiple of 16; kBN for an MN-major B)
+  int RT, NT, KB, KS, kbs, units;
+  int32_t* status;
+  int clear;                  // the call's first kernel: clear the status word
+  // kLse, kDl
+  float scale;                // 1 / tau
+  const int32_t* entry;       // [R][E] vocabulary entries of each token's target, ascending
+  const float* prob;          // [R][E] their probabilities; null: 1
+  int E, V;
+  int v0;                     // first vocabulary entry of the piece
+  float2* part;               // kLse: [NT][R] maximum (in units of log 2) and sum of a tile
+  float* zt;                  // kLse: [R][E] logits (over tau) of the entries
+  const float* lse;           // kDl
+  const float* dloss;         // kDl
+  float gscale;               // kDl: tau
+  __nv_bfloat16* out;         // kDl: ds; kDx (one slot), kDw: the result
+  int64_t ldo;
+  float* out32;               // kDx: fp32 slots [KS][R][N], or null
+  int filled;                 // kDx: slots that pieces before this one have written: add to them
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Shared-memory matrix descriptor of an MN-major operand tile under the 128-byte swizzle: one
+// row of 64 bf16 along M or N per k, 8 k to a 1024-byte swizzle block (stride byte offset), the
+// next 64 along M or N kAtomBytes on (leading byte offset).
+__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF);
+  d |= static_cast<uint64_t>(kAtomBytes >> 4) << 16;
+  d |= static_cast<uint64_t>(1024 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  d |= static_cast<uint64_t>(2) << 61;
+  return d;
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+        "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// A token's ascending entry list, walked along with the columns of a tile.
+struct EntryWalk {
+  const int32_t* e;
+  int k, E, next;
+  __device__ __forceinline__ EntryWalk(const int32_t* list, int E_, int from) : e(list), E(E_) {
+    int lo = 0, hi = E_;
+    while (lo < hi) {                            // first entry >= from
+      const int mid = (lo + hi) >> 1;
+      if (__ldcg(e + mid) < from) lo = mid + 1;
+      else hi = mid;
+    }
+    k = lo;
+    next = k < E ? __ldcg(e + k) : kNone;
+  }
+  __device__ __forceinline__ void step() {
+    ++k;
+    next = k < E ? __ldcg(e + k) : kNone;
+  }
+};
+
+template <int MODE>
+__global__ void __launch_bounds__(kThreads, 1)
+    head_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
+                     const __grid_constant__ CUtensorMap tmB, const GemmArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);
+  uint64_t* empty = full + kStages;
+  uint64_t* tfull = empty + kStages;
+  uint64_t* tempty = tfull + 2;
+  uint64_t* mma_done = tempty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + oMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cid = static_cast<int>(blockIdx.x), ncl = static_cast<int>(gridDim.x);
+  // unit u = (split * NT + column tile) * RT + row tile: the CTAs of a wave share the column
+  // operand's tiles and the row operand stays in L2
+  auto unit_rt = [&](int u) { return u % p.RT; };
+  auto unit_nt = [&](int u) { return (u / p.RT) % p.NT; };
+  auto unit_ks = [&](int u) { return u / p.RT / p.NT; };
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], kEpi);
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmA);
+    prefetch_tmap(&tmB);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_launch_dependents();
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- TMA producer
+    if (lane == 0) {
+      pdl_wait();
+      if (p.clear && blockIdx.x == 0) *p.status = 0;
+      const uint64_t pol = policy_evict_last();
+      const int bn_boxes = b_mn_major(MODE) ? kBN / 64 : 1;
+      const uint32_t bytes =
+          kABytes + (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(p.bn) * kBK * 2);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool issued[kStages];
+      uint32_t parity[kStages];
+#pragma unroll
+      for (int s = 0; s < kStages; ++s) issued[s] = false, parity[s] = 0;
+      for (int u = cid; u < p.units && !*abort_flag; u += ncl) {
+        const int r0 = unit_rt(u) * kBM, n0 = unit_nt(u) * p.bn;
+        const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
+            report(p.status, FQ_ERR_TIMEOUT);
+            *abort_flag = 1;
+            break;
+          }
+          mbar_arrive_expect_tx(&full[stage], bytes);
+          uint8_t* a = smem + oA + stage * kABytes;
+          uint8_t* b = smem + oB + stage * kBBytes;
+          if (a_mn_major(MODE)) {
+#pragma unroll
+            for (int i = 0; i < kBM / 64; ++i)
+              tma_load_2d(a + i * kAtomBytes, &tmA, &full[stage], r0 + 64 * i, kb * kBK, pol);
+          } else {
+            tma_load_2d(a, &tmA, &full[stage], kb * kBK, r0, pol);
+          }
+          if (b_mn_major(MODE)) {
+            for (int i = 0; i < bn_boxes; ++i)
+              tma_load_2d(b + i * kAtomBytes, &tmB, &full[stage], n0 + 64 * i, kb * kBK, pol);
+          } else {
+            tma_load_2d(b, &tmB, &full[stage], kb * kBK, n0, pol);
+          }
+          issued[stage] = true;
+          parity[stage] = phase;
+          if (++stage == kStages) stage = 0, phase ^= 1;
+        }
+      }
+      // never leave with copies in flight
+      for (int s = 0; s < kStages; ++s)
+        if (issued[s] && !mbar_wait(&full[s], parity[s], nullptr))
+          report(p.status, FQ_ERR_TIMEOUT);
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      const uint32_t idesc = umma_idesc_bf16(kBM, static_cast<uint32_t>(p.bn)) |
+                             (a_mn_major(MODE) ? 1u << 15 : 0u) |
+                             (b_mn_major(MODE) ? 1u << 16 : 0u);
+      // 16 k per MMA: 32 bytes along a K-major row, or 16 rows of 128 bytes of an MN-major tile
+      constexpr uint64_t stepA = (a_mn_major(MODE) ? 2048 : 32) >> 4;
+      constexpr uint64_t stepB = (b_mn_major(MODE) ? 2048 : 32) >> 4;
+      int stage = 0, buf = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool issued_any = false;
+      for (int u = cid; u < p.units && !*abort_flag; u += ncl) {
+        const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
+        bool ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
+        tc_fence_after_sync();
+        const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
+        for (int kb = k0; ok && kb < k1; ++kb) {
+          ok = mbar_wait(&full[stage], phase, abort_flag);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t sa = smem_u32(smem + oA + stage * kABytes);
+          const uint32_t sb = smem_u32(smem + oB + stage * kBBytes);
+          const uint64_t ad = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
+          const uint64_t bd = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k)
+            umma_bf16(d, ad + k * stepA, bd + k * stepB, idesc, (kb > k0 || k > 0) ? 1u : 0u);
+          issued_any = true;
+          umma_commit(&empty[stage]);
+          if (++stage == kStages) stage = 0, phase ^= 1;
+        }
+        if (!ok) {
+          report(p.status, FQ_ERR_TIMEOUT);
+          *abort_flag = 1;
+          break;
+        }
+        umma_commit(&tfull[buf]);
+        if (++buf == 2) buf = 0, acc_phase ^= 1;
+      }
+      if (issued_any) {                          // every MMA done before the TMEM is released
+        umma_commit(mma_done);
+        if (!mbar_wait(mma_done, 0, nullptr)) report(p.status, FQ_ERR_TIMEOUT);
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3;
+    const int r_in_tile = quarter * 32 + lane;
+    pdl_wait();
+    int buf = 0;
+    uint32_t acc_phase = 0;
+    for (int u = cid; u < p.units; u += ncl) {
+      const int nt = unit_nt(u);
+      const int row = unit_rt(u) * kBM + r_in_tile, n0 = nt * p.bn;
+      const bool row_ok = row < p.R;
+      const int cols = min(p.bn, p.N - n0);      // valid columns of the tile
+      // the warp leaves as one: the TMEM loads below are warp-wide
+      if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
+        report(p.status, FQ_ERR_TIMEOUT);
+        *abort_flag = 1;
+        break;
+      }
+      tc_fence_after_sync();
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                             static_cast<uint32_t>(buf * kBN);
+      if (MODE == kLse || MODE == kDl) {
+        const int64_t lrow = row_ok ? row : 0;
+        EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, p.v0 + n0);
+        const float c2 = p.scale * kLog2e;
+        float m = -CUDART_INF_F, sum = 0.f;      // running maximum and sum, in units of log 2
+        float lse2 = 0.f, g = 0.f;
+        bool has = false;
+        if (MODE == kDl && row_ok) {
+          const int first = __ldcg(p.entry + lrow * p.E);
+          has = first >= 0 && first < p.V;
+          lse2 = __ldcg(p.lse + row) * kLog2e;
+          g = __ldcg(p.dloss + row) * p.gscale;
+        }
+#pragma unroll 1
+        for (int c = 0; c < cols; c += kChunk) {
+          float v[kChunk];
+          __syncwarp();
+          tmem_ld32(t_row + c, v);
+          tmem_wait_ld();
+          if (MODE == kLse) {
+            while (w.next < p.v0 + n0 + c + kChunk && w.next < p.v0 + n0 + cols) {
+              const int j = w.next - (p.v0 + n0 + c);
+              float z = 0.f;
+#pragma unroll
+              for (int q = 0; q < kChunk; ++q) z = q == j ? v[q] : z;
+              p.zt[lrow * p.E + w.k] = z * p.scale;
+              w.step();
+            }
+            float cm = -CUDART_INF_F;
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) {
+              v[q] = c + q < cols ? v[q] * c2 : -CUDART_INF_F;
+              cm = fmaxf(cm, v[q]);
+            }
+            const float mn = fmaxf(m, cm);
+            const float ref = mn == -CUDART_INF_F ? 0.f : mn;
+            float s = 0.f;
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) s += ex2(v[q] - ref);
+            sum = fmaf(sum, ex2(m - ref), s);
+            m = mn;
+          } else {
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) v[q] = ex2(fmaf(v[q], c2, -lse2));
+            while (w.next < p.v0 + n0 + c + kChunk) {
+              const int j = w.next - (p.v0 + n0 + c);
+              const float pk = p.prob ? __ldcg(p.prob + lrow * p.E + w.k) : 1.f;
+#pragma unroll
+              for (int q = 0; q < kChunk; ++q) v[q] -= q == j ? pk : 0.f;
+              w.step();
+            }
+            if (row_ok) {
+              uint4* dst = reinterpret_cast<uint4*>(p.out + row * p.ldo + n0 + c);
+#pragma unroll
+              for (int q = 0; q < kChunk; q += 8) {
+                if (c + q >= p.bn) break;        // the next tile's columns
+                uint4 o;
+                o.x = has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u;
+                o.y = has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u;
+                o.z = has ? pack_bf16(g * v[q + 4], g * v[q + 5]) : 0u;
+                o.w = has ? pack_bf16(g * v[q + 6], g * v[q + 7]) : 0u;
+                dst[q / 8] = o;
+              }
+            }
+          }
+        }
+        if (MODE == kLse && row_ok)
+          p.part[static_cast<int64_t>(nt) * p.R + row] = make_float2(m, sum);
+      } else {
+        // result rows; N is a multiple of 8
+        float* o32 = p.out32 ? p.out32 + (static_cast<int64_t>(unit_ks(u)) * p.R + row) * p.N + n0
+                             : nullptr;
+        __nv_bfloat16* o16 = p.out + static_cast<int64_t>(row) * p.ldo + n0;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += kChunk) {
+          float v[kChunk];
+          __syncwarp();
+          tmem_ld32(t_row + c, v);
+          tmem_wait_ld();
+          if (!row_ok) continue;
+#pragma unroll
+          for (int q = 0; q < kChunk; q += 8) {
+            if (c + q >= cols) break;
+            if (MODE == kDx && o32) {
+#pragma unroll
+              for (int h = 0; h < 8; h += 4) {
+                float4* dst = reinterpret_cast<float4*>(o32 + c + q + h);
+                float4 o = make_float4(v[q + h], v[q + h + 1], v[q + h + 2], v[q + h + 3]);
+                if (unit_ks(u) < p.filled) {
+                  const float4 old = *dst;
+                  o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+                }
+                *dst = o;
+              }
+            } else {
+              uint4 o;
+              o.x = pack_bf16(v[q], v[q + 1]);
+              o.y = pack_bf16(v[q + 2], v[q + 3]);
+              o.z = pack_bf16(v[q + 4], v[q + 5]);
+              o.w = pack_bf16(v[q + 6], v[q + 7]);
+              *reinterpret_cast<uint4*>(o16 + c + q) = o;
+            }
+          }
+        }
+      }
+      tc_fence_before_sync();
+      mbar_arrive(&tempty[buf]);
+      if (++buf == 2) buf = 0, acc_phase ^= 1;
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// An entry of a teacher's list counts when its index is one of the vocabulary and its logit is
+// above -inf (a NaN counts, and shows in the loss).
+__device__ __forceinline__ bool entry_counts(int32_t index, float logit, int V) {
+  return index >= 0 && index < V && !(logit == -CUDART_INF_F);
+}
+
+// One block per token: the teacher's probabilities of its entries, in ascending order of the
+// vocabulary entry (rank of each entry by counting, K <= 1024), entries that do not count last;
+// and sum_k p_k log p_k.
+constexpr int kSortThreads = 128;
+
+__global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
+    const int32_t* index, const float* logit, int K, int V, float inv_tau, int32_t* entry,
+    float* prob, float* plogp, int32_t* status) {
+  __shared__ int32_t idx[FQ_DISTILL_MAX_K];
+  __shared__ float tl[FQ_DISTILL_MAX_K];
+  __shared__ float red[kSortThreads / 32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * K;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  float top = -CUDART_INF_F;
+  for (int k = threadIdx.x; k < K; k += kSortThreads) {
+    const int32_t i = __ldcg(index + base + k);
+    const float t = __ldcg(logit + base + k);
+    const bool ok = entry_counts(i, t, V);
+    idx[k] = ok ? i : kNone;
+    tl[k] = ok ? t * inv_tau : -CUDART_INF_F;
+    top = fmaxf(top, tl[k]);
+  }
+  top = warp_max(top);
+  if (lane == 0) red[warp] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  __syncthreads();
+  const float ref = top == -CUDART_INF_F ? 0.f : top;
+  float s = 0.f;
+  for (int k = threadIdx.x; k < K; k += kSortThreads) s += expf(tl[k] - ref);
+  s = warp_sum(s);
+  if (lane == 0) red[warp] = s;
+  __syncthreads();
+  s = (red[0] + red[1]) + (red[2] + red[3]);
+  __syncthreads();
+  const float logs = logf(s);
+  float h = 0.f;
+  for (int k = threadIdx.x; k < K; k += kSortThreads) {
+    const int32_t i = idx[k];
+    int rank = 0;
+    for (int j = 0; j < K; ++j) rank += idx[j] < i || (idx[j] == i && j < k);
+    const float pk = i == kNone ? 0.f : expf(tl[k] - ref) / s;
+    if (i != kNone && !(pk == 0.f)) h += pk * (tl[k] - ref - logs);
+    entry[base + rank] = i;
+    prob[base + rank] = pk;
+  }
+  h = warp_sum(h);
+  if (lane == 0) red[warp] = h;
+  __syncthreads();
+  if (threadIdx.x == 0) plogp[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// One warp per token: joins the tiles' maxima and sums, then the loss.  Reports targets beyond
+// the vocabulary.
+constexpr int kJoinWarps = 4;
+
+__global__ void __launch_bounds__(32 * kJoinWarps) head_join_kernel(
+    const float2* part, int NT, int M, int V, const int32_t* given, const int32_t* entry,
+    const float* prob, const float* zt, const float* plogp, int E, float tau2, float* loss,
+    float* lse, int32_t* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int row = blockIdx.x * kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (row >= M) return;
+  const int64_t base = static_cast<int64_t>(row) * E;
+  bool bad = false;
+  for (int k = lane; k < E; k += 32) bad |= __ldcg(given + base + k) >= V;
+  if (__any_sync(0xffffffffu, bad) && lane == 0) report(status, FQ_ERR_DEVICE_CHECK);
+  float m = -CUDART_INF_F, s = 0.f;
+  for (int t = lane; t < NT; t += 32) {
+    const float2 q = __ldcg(part + static_cast<int64_t>(t) * M + row);
+    const float mn = fmaxf(m, q.x);
+    const float ref = mn == -CUDART_INF_F ? 0.f : mn;
+    s = s * exp2f(m - ref) + q.y * exp2f(q.x - ref);
+    m = mn;
+  }
+  const float top = warp_max(m);
+  const float ref = top == -CUDART_INF_F ? 0.f : top;
+  s = warp_sum(s * exp2f(m - ref));
+  const float l = (ref + log2f(s)) * kLn2;
+  float d = 0.f;
+  for (int k = lane; k < E; k += 32) {
+    const int32_t i = __ldcg(entry + base + k);
+    if (i < 0 || i >= V) continue;
+    const float pk = prob ? __ldcg(prob + base + k) : 1.f;
+    d += pk == 0.f ? 0.f : pk * (l - __ldcg(zt + base + k));
+  }
+  d = warp_sum(d);
+  if (lane == 0) {
+    const int32_t first = __ldcg(entry + base);
+    const bool has = first >= 0 && first < V;
+    loss[row] = has ? tau2 * (d + (plogp ? __ldcg(plogp + row) : 0.f)) : 0.f;
+    lse[row] = has ? l : 0.f;
+  }
+}
+
+// Copy of x with the rows of tokens without a target cleared, so that what such a row holds
+// (infinities, NaN) meets no product with its zero gradient.  One block per token.  Clears
+// *status where it is the call's first kernel (else null).
+__global__ void __launch_bounds__(256) head_mask_rows_kernel(const uint4* x, int d8,
+                                                             const int32_t* entry, int E, int V,
+                                                             uint4* xc, int32_t* status) {
+  pdl_launch_dependents();
+  pdl_wait();
+  if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  const int64_t row = blockIdx.x;
+  const int32_t first = __ldcg(entry + row * E);
+  const bool has = first >= 0 && first < V;
+  for (int j = threadIdx.x; j < d8; j += blockDim.x)
+    xc[row * d8 + j] = has ? __ldcg(x + row * d8 + j) : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// dx from its fp32 slots, added in slot order.
+__global__ void __launch_bounds__(256) head_dx_kernel(const float4* slots, int S, int64_t n4,
+                                                      uint2* dx) {
+  pdl_launch_dependents();
+  pdl_wait();
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n4; i += 256ll * gridDim.x) {
+    float4 a = __ldcg(slots + i);
+    for (int s = 1; s < S; ++s) {
+      const float4 b = __ldcg(slots + s * n4 + i);
+      a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
+    }
+    dx[i] = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000,
+                                         cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+  });
+  return fn;
+}
+
+// bf16 matrix rows x cols with a row pitch of ld elements, boxes of 64 columns x box_rows rows
+// under the 128-byte swizzle
+bool make_tmap(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld,
+               int box_rows) {
+  auto enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2};
+  cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int sm_count() {
+  int dev = 0, n = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+  return n > 0 ? n : 148;
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem,
+                   cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(block));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int MODE>
+fq_status launch_gemm(const CUtensorMap& a, const CUtensorMap& b, GemmArgs& g, int sms,
+                      cudaStream_t s) {
+  static std::mutex mu;
+  static std::map<int, bool> done;
+  {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!done[dev]) {
+      if (cudaFuncSetAttribute(head_gemm_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               kSmemBytes) != cudaSuccess)
+        return FQ_ERR_CUDA;
+      done[dev] = true;
+    }
+  }
+  return launch(head_gemm_kernel<MODE>, std::min(g.units, sms), kThreads, kSmemBytes, s, a, b,
+                g) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+void plan(GemmArgs& g, int R, int N, int K, int bn, int splits) {
+  g.R = R;
+  g.N = N;
+  g.K = K;
+  g.bn = bn;
+  g.RT = static_cast<int>(ceil_div(R, kBM));
+  g.NT = static_cast<int>(ceil_div(N, bn));
+  g.KB = static_cast<int>(ceil_div(K, kBK));
+  g.kbs = static_cast<int>(ceil_div(g.KB, splits));
+  g.KS = static_cast<int>(ceil_div(g.KB, g.kbs));
+  g.units = g.RT * g.NT * g.KS;
+}
+
+// Columns per tile of the logit products: the width whose rounds of tiles over the SMs take the
+// least time (a tile's time is proportional to its width), the widest of equals.
+int pick_bn(int R, int N, int sms) {
+  const int64_t RT = ceil_div(R, kBM);
+  int best = kBN;
+  int64_t cost = -1;
+  for (int bn = kBN; bn >= 128; bn -= 16) {
+    const int64_t c = ceil_div(RT * ceil_div(N, bn), sms) * bn;
+    if (cost < 0 || c < cost) cost = c, best = bn;
+  }
+  return best;
+}
+
+constexpr int kMinBn = 128;
+constexpr int64_t kPieceBytes = 128ll << 20;    // ds of one piece of the vocabulary
+constexpr int kMinPiece = 2048;
+constexpr int kMaxSlots = 16;                   // fp32 slots of a dx split over the vocabulary
+constexpr int kMaxSms = 256;                    // bound on the SM count used for planning
+
+// Vocabulary entries per piece: as many as kPieceBytes of ds hold (at least kMinPiece), in
+// pieces of equal size rounded up to 256.
+int piece_width(int M, int V) {
+  const int64_t most = std::max<int64_t>(kMinPiece, kPieceBytes / 2 / M);
+  const int64_t n = ceil_div(V, most);
+  return static_cast<int>(std::min<int64_t>(round_up(V, 256), round_up(ceil_div(V, n), 256)));
+}
+
+// Ways the contraction of dx over a piece is split, so that few tiles still fill the SMs.
+int dx_splits(int M, int d, int Vc, int sms) {
+  const int64_t tiles = ceil_div(M, kBM) * ceil_div(d, kBN);
+  const int64_t KB = ceil_div(Vc, kBK);
+  return static_cast<int>(std::max<int64_t>(
+      1, std::min<int64_t>({kMaxSlots, std::min(sms, kMaxSms) / tiles, KB / 8})));
+}
+
+struct Ws {
+  size_t entry, prob, plogp, zt, part, xc, ds, slots, total;
+};
+
+Ws ws_layout(int M, int d, int V, int K, bool grad) {
+  Ws L{};
+  size_t off = kWsHeader;
+  auto take = [&](size_t n) {
+    const size_t at = off;
+    off += static_cast<size_t>(round_up(static_cast<int64_t>(n), 256));
+    return at;
+  };
+  const size_t mk = static_cast<size_t>(M) * K * 4;
+  L.entry = take(mk);
+  L.prob = take(mk);
+  L.plogp = take(static_cast<size_t>(M) * 4);
+  if (!grad) {
+    L.zt = take(mk);
+    L.part = take(static_cast<size_t>(ceil_div(V, kMinBn)) * M * 8);
+  } else {
+    const int P = piece_width(M, V);
+    L.xc = take(static_cast<size_t>(M) * d * 2);
+    // the pitch leaves room for the last tile's columns beyond the piece
+    L.ds = take(static_cast<size_t>(M) * (P + kBN) * 2);
+    // sized for any SM count
+    const int S = dx_splits(M, d, std::min(P, V), kMaxSms);
+    L.slots = take(S > 1 || P < V ? static_cast<size_t>(S) * M * d * 4 : 0);
+  }
+  L.total = off;
+  return L;
+}
+
+struct Target {
+  const int32_t* given;       // target (M) or index (M x K)
+  const float* logit;         // distillation, else null
+  int K;
+  float tau;
+};
+
+fq_status check_common(const void* x, int M, int d, const void* W, int V, const Target& t,
+                       const void* lse, size_t need, const void* ws, size_t ws_bytes) {
+  if (!x || !W || !t.given || !lse || M <= 0 || d <= 0 || V <= 0) return FQ_ERR_INVALID_ARG;
+  if (t.K < 1 || t.K > FQ_DISTILL_MAX_K || !(t.tau > 0.f) || !std::isfinite(t.tau))
+    return FQ_ERR_INVALID_ARG;
+  if (d % 8 || !aligned16(x) || !aligned16(W) || !aligned16(t.given) || !aligned16(t.logit) ||
+      !aligned16(lse))
+    return FQ_ERR_ALIGNMENT;
+  if (!ws) return FQ_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return FQ_ERR_ALIGNMENT;
+  if (need == 0) return FQ_ERR_INVALID_ARG;
+  if (ws_bytes < need) return FQ_ERR_WORKSPACE;
+  return FQ_OK;
+}
+
+fq_status check_device() {
+  int dev = 0, major = 0, minor = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+    return FQ_ERR_CUDA;
+  return major * 10 + minor == 103 ? FQ_OK : FQ_ERR_UNSUPPORTED;
+}
+
+// The token's entries in ascending order: the target itself, or the sorted teacher's list.
+fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws,
+                         const int32_t*& entry, const float*& prob, const float*& plogp,
+                         cudaStream_t s) {
+  if (!t.logit) {
+    entry = t.given;
+    prob = plogp = nullptr;
+    return FQ_OK;
+  }
+  auto* e = reinterpret_cast<int32_t*>(ws + L.entry);
+  auto* pr = reinterpret_cast<float*>(ws + L.prob);
+  auto* pl = reinterpret_cast<float*>(ws + L.plogp);
+  entry = e;
+  prob = pr;
+  plogp = pl;
+  return launch(head_entries_kernel, M, kSortThreads, 0, s, t.given, t.logit, t.K, V,
+                1.f / t.tau, e, pr, pl, reinterpret_cast<int32_t*>(ws)) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Target& t,
+                    float* loss, float* lse, void* wsv, size_t ws_bytes, cudaStream_t s) {
+  if (const fq_status st = check_common(x, M, d, W, V, t, lse,
+                                        fq_head_workspace_bytes(M, d, V, t.K), wsv, ws_bytes))
+    return st;
+  if (!loss) return FQ_ERR_INVALID_ARG;
+  if (!aligned16(loss)) return FQ_ERR_ALIGNMENT;
+  if (const fq_status st = check_device()) return st;
+  const Ws L = ws_layout(M, d, V, t.K, false);
+  char* ws = static_cast<char*>(wsv);
+  const int sms = sm_count();
+  GemmArgs g{};
+  plan(g, M, V, d, pick_bn(M, V, sms), 1);
+  CUtensorMap mx, mw;
+  if (!make_tmap(&mx, x, M, d, d, kBM) || !make_tmap(&mw, W, V, d, d, g.bn)) return FQ_ERR_CUDA;
+  const float* plogp = nullptr;
+  if (const fq_status st = launch_entries(t, M, V, L, ws, g.entry, g.prob, plogp, s)) return st;
+  g.status = reinterpret_cast<int32_t*>(ws);
+  g.clear = t.logit == nullptr;
+  g.scale = 1.f / t.tau;
+  g.E = t.K;
+  g.V = V;
+  g.part = reinterpret_cast<float2*>(ws + L.part);
+  g.zt = reinterpret_cast<float*>(ws + L.zt);
+  if (const fq_status st = launch_gemm<kLse>(mx, mw, g, sms, s)) return st;
+  return launch(head_join_kernel, ceil_div(M, kJoinWarps), 32 * kJoinWarps, 0, s,
+                static_cast<const float2*>(g.part), g.NT, M, V, t.given, g.entry, g.prob,
+                static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, loss,
+                lse, g.status) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Target& t,
+                    const float* lse, const float* dloss, void* dx, void* dW, void* wsv,
+                    size_t ws_bytes, cudaStream_t s) {
+  if (const fq_status st =
+          check_common(x, M, d, W, V, t, lse, fq_head_grad_workspace_bytes(M, d, V, t.K), wsv,
+                       ws_bytes))
+    return st;
+  if (!dloss || (!dx && !dW)) return FQ_ERR_INVALID_ARG;
+  if (!aligned16(dloss) || !aligned16(dx) || !aligned16(dW)) return FQ_ERR_ALIGNMENT;
+  if (const fq_status st = check_device()) return st;
+  const Ws L = ws_layout(M, d, V, t.K, true);
+  char* ws = static_cast<char*>(wsv);
+  const int sms = sm_count();
+  auto* status = reinterpret_cast<int32_t*>(ws);
+  auto* xc = reinterpret_cast<__nv_bfloat16*>(ws + L.xc);
+  auto* ds = reinterpret_cast<__nv_bfloat16*>(ws + L.ds);
+  auto* slots = reinterpret_cast<float*>(ws + L.slots);
+  const auto* Wb = static_cast<const __nv_bfloat16*>(W);
+
+  const int32_t* entry = nullptr;
+  const float *prob = nullptr, *plogp = nullptr;
+  if (const fq_status st = launch_entries(t, M, V, L, ws, entry, prob, plogp, s)) return st;
+  if (launch(head_mask_rows_kernel, M, 256, 0, s, static_cast<const uint4*>(x), d / 8, entry, t.K,
+             V, reinterpret_cast<uint4*>(xc), t.logit ? nullptr : status) != cudaSuccess)
+    return FQ_ERR_CUDA;
+
+  const int P = piece_width(M, V);
+  const int pieces = static_cast<int>(ceil_div(V, P));
+  const int64_t ldds = P + kBN;
+  const int splits = dx_splits(M, d, std::min(P, V), sms);
+  const bool direct = splits == 1 && pieces == 1;
+  int used = 0;
+  for (int q = 0; q < pieces; ++q) {
+    const int v0 = q * P, Vc = std::min(P, V - v0);
+    const __nv_bfloat16* Wq = Wb + static_cast<int64_t>(v0) * d;
+    CUtensorMap mx, mw;
+    {
+      GemmArgs g{};
+      plan(g, M, Vc, d, pick_bn(M, Vc, sms), 1);
+      if (!make_tmap(&mx, xc, M, d, d, kBM) || !make_tmap(&mw, Wq, Vc, d, d, g.bn))
+        return FQ_ERR_CUDA;
+      g.status = status;
+      g.scale = 1.f / t.tau;
+      g.entry = entry;
+      g.prob = prob;
+      g.E = t.K;
+      g.V = V;
+      g.v0 = v0;
+      g.lse = lse;
+      g.dloss = dloss;
+      g.gscale = t.logit ? t.tau : 1.f;
+      g.out = ds;
+      g.ldo = ldds;
+      if (const fq_status st = launch_gemm<kDl>(mx, mw, g, sms, s)) return st;
+    }
+    CUtensorMap ma, mb;
+    if (dx) {
+      GemmArgs g{};
+      plan(g, M, d, Vc, kBN, splits);
+      if (!make_tmap(&ma, ds, M, Vc, ldds, kBM) || !make_tmap(&mb, Wq, Vc, d, d, kBK))
+        return FQ_ERR_CUDA;
+      g.status = status;
+      g.out = static_cast<__nv_bfloat16*>(dx);
+      g.ldo = d;
+      g.out32 = direct ? nullptr : slots;
+      g.filled = used;
+      used = std::max(used, g.KS);
+      if (const fq_status st = launch_gemm<kDx>(ma, mb, g, sms, s)) return st;
+    }
+    if (dW) {
+      GemmArgs g{};
+      plan(g, Vc, d, M, kBN, 1);
+      if (!make_tmap(&ma, ds, M, Vc, ldds, kBK) || !make_tmap(&mb, xc, M, d, d, kBK))
+        return FQ_ERR_CUDA;
+      g.status = status;
+      g.out = static_cast<__nv_bfloat16*>(dW) + static_cast<int64_t>(v0) * d;
+      g.ldo = d;
+      if (const fq_status st = launch_gemm<kDw>(ma, mb, g, sms, s)) return st;
+    }
+  }
+  if (dx && !direct) {
+    const int64_t n4 = static_cast<int64_t>(M) * d / 4;
+    if (launch(head_dx_kernel, std::min<int64_t>(ceil_div(n4, 256), 8ll * sms), 256, 0, s,
+               reinterpret_cast<const float4*>(slots), used, n4,
+               static_cast<uint2*>(dx)) != cudaSuccess)
+      return FQ_ERR_CUDA;
+  }
+  return FQ_OK;
+}
+
+}  // namespace
+}  // namespace fq
+
+using namespace fq;
+
+extern "C" {
+
+size_t fq_head_workspace_bytes(int M, int d, int V, int K) {
+  if (M <= 0 || d <= 0 || V <= 0 || K < 1 || K > FQ_DISTILL_MAX_K) return 0;
+  return ws_layout(M, d, V, K, false).total;
+}
+
+size_t fq_head_grad_workspace_bytes(int M, int d, int V, int K) {
+  if (M <= 0 || d <= 0 || V <= 0 || K < 1 || K > FQ_DISTILL_MAX_K) return 0;
+  return ws_layout(M, d, V, K, true).total;
+}
+
+fq_status fq_cross_entropy(const void* x, int M, int d, const void* W, int V,
+                           const int32_t* target, float* loss, float* lse, void* ws,
+                           size_t ws_bytes, fq_stream_t stream) {
+  return head_loss(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, loss, lse, ws, ws_bytes,
+                   reinterpret_cast<cudaStream_t>(stream));
+}
+
+fq_status fq_cross_entropy_grad(const void* x, int M, int d, const void* W, int V,
+                                const int32_t* target, const float* lse, const float* dloss,
+                                void* dx, void* dW, void* ws, size_t ws_bytes,
+                                fq_stream_t stream) {
+  return head_grad(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, lse, dloss, dx, dW, ws,
+                   ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+fq_status fq_distill(const void* x, int M, int d, const void* W, int V, const int32_t* index,
+                     const float* logit, int K, float tau, float* loss, float* lse, void* ws,
+                     size_t ws_bytes, fq_stream_t stream) {
+  if (!logit) return FQ_ERR_INVALID_ARG;
+  return head_loss(x, M, d, W, V, Target{index, logit, K, tau}, loss, lse, ws, ws_bytes,
+                   reinterpret_cast<cudaStream_t>(stream));
+}
+
+fq_status fq_distill_grad(const void* x, int M, int d, const void* W, int V,
+                          const int32_t* index, const float* logit, int K, float tau,
+                          const float* lse, const float* dloss, void* dx, void* dW, void* ws,
+                          size_t ws_bytes, fq_stream_t stream) {
+  if (!logit) return FQ_ERR_INVALID_ARG;
+  return head_grad(x, M, d, W, V, Target{index, logit, K, tau}, lse, dloss, dx, dW, ws, ws_bytes,
+                   reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
