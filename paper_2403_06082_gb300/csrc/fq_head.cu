@@ -2,20 +2,29 @@
 // tensor cores, without keeping the logits.
 //
 // One persistent, warp-specialised kernel computes tiles of  acc[i][j] = sum_k A[i][k] B[j][k]
-// (128 rows of A on the tensor core's rows, bn <= 256 rows of B on its columns, fp32 in TMEM)
-// for the four products of a training step:
+// (CG * 128 rows of A on the tensor cores' rows, bn <= 256 rows of B on their columns, fp32 in
+// TMEM) for the four products of a training step:
 //   kLse  A = x (tokens),   B = W (vocabulary),  k = d: per token and tile the running maximum
 //         and sum of exponentials, and the logits of the token's targets;
 //   kDl   the same product again: ds = g (softmax - target) as bf16, one piece of the vocabulary;
 //   kDx   A = ds (tokens),  B = W^T (d columns), k = the piece: dx;
 //   kDw   A = ds^T (vocabulary rows), B = x^T (d columns), k = tokens: dW of the piece.
-// A token is a row of the accumulator, i.e. one epilogue thread, so the softmax statistics of a
-// tile need no exchange between threads.  Operands whose contraction dimension is not the
+// A token is a row of the accumulator, i.e. one epilogue thread per half row, so the softmax
+// statistics need no exchange between threads.  Operands whose contraction dimension is not the
 // contiguous one (W in kDx, ds and x in kDw) are read as they lie in memory, as MN-major tiles:
 // nothing is transposed.
 //
-// Warp roles: warp 0 TMA producer (one lane), warp 1 TMEM owner + MMA issuer (one lane),
-// warps 2-5 epilogue (thread = accumulator row).
+// With CG = 2 a cluster of two CTAs works on one tile of 256 x bn: each CTA stages its 128 rows
+// of A and half of the rows of B, one MMA reads both CTAs' shared memory, and each CTA finishes
+// its own 128 rows.  Against one CTA per 128 x 256 tile this halves the reads of B per SM.
+// Results of at most 128 rows take CG = 1.
+//
+// kLse adds the accumulator up in registers every kSegBlocks k-blocks.  The tensor core cuts off
+// what is below its accumulator's last bit at every step, so a long sum drifts towards zero: at
+// d = 4096 the loss was off by 1.9e-6 of its norm against 4e-7 for fp32 products.
+//
+// Warp roles: warp 0 TMA producer (one lane), warp 1 TMEM owner + MMA issuer (one lane, of the
+// first CTA of a pair), warps 2-9 epilogue (thread = half an accumulator row).
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -34,27 +43,34 @@ namespace {
 
 enum Mode : int { kLse = 0, kDl = 1, kDx = 2, kDw = 3 };
 
-constexpr int kBM = 128;                        // accumulator rows per tile
+constexpr int kBM = 128;                        // accumulator rows per CTA
 constexpr int kBN = 256;                        // accumulator columns per tile, at most
 constexpr int kBK = 64;                         // k per stage: one 128-byte swizzle row of bf16
 constexpr int kABytes = kBM * kBK * 2;
-constexpr int kBBytes = kBN * kBK * 2;
 constexpr int kAtomBytes = 64 * kBK * 2;        // MN-major: 64 rows of the operand x kBK
-constexpr int kStages = 4;
-constexpr int kThreads = 192;
-constexpr int kEpi = 128;
+constexpr int kThreads = 320;
+constexpr int kEpiWarps = 8;
 constexpr int kChunk = 32;                      // accumulator columns per epilogue step
+constexpr int kMinBn = 32;
+constexpr int kMaxSms = 256;                    // bound on the SM count used for planning
+constexpr int kHalf = 128;                      // accumulator columns of an epilogue thread
+constexpr int kSegBlocks = 16;                  // kLse: k blocks per accumulator in TMEM
 constexpr int kTmemCols = 2 * kBN;
 constexpr int kNone = 0x7fffffff;               // sorted entry lists: no entry
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-constexpr int oA = 0;
-constexpr int oB = oA + kStages * kABytes;
-constexpr int oBar = oB + kStages * kBBytes;
-constexpr int oMisc = oBar + (2 * kStages + 5) * 8;
-constexpr int kSmemBytes = oMisc + 16 + 1024;   // + alignment slack
-static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+template <int CG>
+struct Lay {
+  static constexpr int kBBytes = kBN / CG * kBK * 2;          // this CTA's rows of B
+  static constexpr int kStages = CG == 2 ? 6 : 4;
+  static constexpr int oA = 0;
+  static constexpr int oB = oA + kStages * kABytes;
+  static constexpr int oBar = oB + kStages * kBBytes;
+  static constexpr int oMisc = oBar + (2 * kStages + 4) * 8;
+  static constexpr int kBytes = oMisc + 16 + 1024;            // + alignment slack
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
 
 constexpr bool a_mn_major(int mode) { return mode == kDw; }
 constexpr bool b_mn_major(int mode) { return mode == kDx || mode == kDw; }
@@ -65,13 +81,14 @@ struct GemmArgs {
   int RT, NT, KB, KS, kbs, units;
   int32_t* status;
   int clear;                  // the call's first kernel: clear the status word
+  int a_rows;                 // K-major A: rows per copy (fewer than kBM where R is)
   // kLse, kDl
   float scale;                // 1 / tau
   const int32_t* entry;       // [R][E] vocabulary entries of each token's target, ascending
   const float* prob;          // [R][E] their probabilities; null: 1
   int E, V;
   int v0;                     // first vocabulary entry of the piece
-  float2* part;               // kLse: [NT][R] maximum (in units of log 2) and sum of a tile
+  float2* part;               // kLse: [2 NT][R] maximum (in units of log 2) and sum of half a tile
   float* zt;                  // kLse: [R][E] logits (over tau) of the entries
   const float* lse;           // kDl
   const float* dloss;         // kDl
@@ -143,23 +160,97 @@ struct EntryWalk {
   }
 };
 
-template <int MODE>
+// Arrive on an mbarrier of any CTA of the cluster (address from mapa).  No cluster-wide release:
+// what the arrival orders is TMEM reads, by the tcgen05 fence before it, and a release at cluster
+// scope stalls for about a thousand cycles (with one per stage the kernel ran at 620 TFLOP/s).
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// 2-D TMA load of one CTA of a pair; the bytes count on an mbarrier of the pair's first CTA.
+__device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const void* tmap, uint32_t bar,
+                                                 int32_t x, int32_t y, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile"
+      ".mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;" ::"r"(
+          smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y), "l"(policy)
+      : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tmem_alloc_cg(uint32_t* smem_dst, uint32_t ncols) {
+  if constexpr (CG == 1) {
+    tmem_alloc(smem_dst, ncols);
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(smem_dst)),
+                 "r"(ncols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+
+template <int CG>
+__device__ __forceinline__ void tmem_dealloc_cg(uint32_t taddr, uint32_t ncols) {
+  if constexpr (CG == 1) {
+    tmem_dealloc(taddr, ncols);
+  } else {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr),
+                 "r"(ncols)
+                 : "memory");
+  }
+}
+
+template <int CG>
+__device__ __forceinline__ void umma_cg(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
+                                        uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CG == 1) {
+    umma_bf16(tmem_d, adesc, bdesc, idesc, accumulate);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  }
+}
+
+// Arrive on the mbarrier at this offset (of both CTAs of a pair) once every MMA issued so far by
+// this thread has completed.
+template <int CG>
+__device__ __forceinline__ void umma_commit_cg(uint64_t* bar) {
+  if constexpr (CG == 1) {
+    umma_commit(bar);
+  } else {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;" ::"r"(smem_u32(bar)),
+        "h"(static_cast<uint16_t>(3))
+        : "memory");
+  }
+}
+
+template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1)
     head_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                      const __grid_constant__ CUtensorMap tmB, const GemmArgs p) {
+  using Lo = Lay<CG>;
+  constexpr int kStages = Lo::kStages, kBBytes = Lo::kBBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Lo::oBar);   // used in the pair's first CTA
   uint64_t* empty = full + kStages;
   uint64_t* tfull = empty + kStages;
-  uint64_t* tempty = tfull + 2;
-  uint64_t* mma_done = tempty + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + oMisc);
+  uint64_t* tempty = tfull + 2;                                    // used in the pair's first CTA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + Lo::oMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int cid = static_cast<int>(blockIdx.x), ncl = static_cast<int>(gridDim.x);
+  const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int cid = static_cast<int>(blockIdx.x) / CG, ncl = static_cast<int>(gridDim.x) / CG;
   // unit u = (split * NT + column tile) * RT + row tile: the CTAs of a wave share the column
   // operand's tiles and the row operand stays in L2
   auto unit_rt = [&](int u) { return u % p.RT; };
@@ -173,17 +264,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], kEpi);
+      mbar_init(&tempty[b], CG * kEpiWarps);
     }
-    mbar_init(mma_done, 1);
     *abort_flag = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA);
     prefetch_tmap(&tmB);
   }
-  if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+  if (warp == 1) tmem_alloc_cg<CG>(tmem_slot, kTmemCols);
   tc_fence_before_sync();
   __syncthreads();
+  if (CG == 2) cluster_sync();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
@@ -194,54 +285,64 @@ __global__ void __launch_bounds__(kThreads, 1)
       pdl_wait();
       if (p.clear && blockIdx.x == 0) *p.status = 0;
       const uint64_t pol = policy_evict_last();
-      const int bn_boxes = b_mn_major(MODE) ? kBN / 64 : 1;
+      const int bn_cta = p.bn / CG;                 // rows of B of this CTA
       const uint32_t bytes =
-          kABytes + (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(p.bn) * kBK * 2);
+          (a_mn_major(MODE) ? kABytes : static_cast<uint32_t>(p.a_rows) * kBK * 2) +
+          (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(bn_cta) * kBK * 2);
+      // a B that is read once (one row tile) need not stay in L2
+      const uint64_t pol_b = p.RT == 1 ? policy_evict_first() : pol;
       int stage = 0;
       uint32_t phase = 0;
-      bool issued[kStages];
-      uint32_t parity[kStages];
-#pragma unroll
-      for (int s = 0; s < kStages; ++s) issued[s] = false, parity[s] = 0;
+      int64_t it = 0;
       for (int u = cid; u < p.units && !*abort_flag; u += ncl) {
-        const int r0 = unit_rt(u) * kBM, n0 = unit_nt(u) * p.bn;
+        const int r0 = (unit_rt(u) * CG + rank) * kBM;
+        const int n0 = unit_nt(u) * p.bn + rank * bn_cta;
         const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
-        for (int kb = k0; kb < k1; ++kb) {
+        for (int kb = k0; kb < k1; ++kb, ++it) {
           if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
             report(p.status, FQ_ERR_TIMEOUT);
             *abort_flag = 1;
             break;
           }
-          mbar_arrive_expect_tx(&full[stage], bytes);
-          uint8_t* a = smem + oA + stage * kABytes;
-          uint8_t* b = smem + oB + stage * kBBytes;
+          uint8_t* a = smem + Lo::oA + stage * kABytes;
+          uint8_t* b = smem + Lo::oB + stage * kBBytes;
+          const uint32_t lead = CG == 2 ? mapa(smem_u32(&full[stage]), 0) : 0;
+          // The first CTA expects the bytes of both.  The other's may arrive before it does: the
+          // phase still waits for the one arrival.
+          if (rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
+          auto load = [&](uint8_t* dst, const CUtensorMap* tm, int cx, int cy, uint64_t pl) {
+            if (CG == 2) tma_load_2d_pair(dst, tm, lead, cx, cy, pl);
+            else tma_load_2d(dst, tm, &full[stage], cx, cy, pl);
+          };
           if (a_mn_major(MODE)) {
 #pragma unroll
             for (int i = 0; i < kBM / 64; ++i)
-              tma_load_2d(a + i * kAtomBytes, &tmA, &full[stage], r0 + 64 * i, kb * kBK, pol);
+              load(a + i * kAtomBytes, &tmA, r0 + 64 * i, kb * kBK, pol);
           } else {
-            tma_load_2d(a, &tmA, &full[stage], kb * kBK, r0, pol);
+            load(a, &tmA, kb * kBK, r0, pol);
           }
           if (b_mn_major(MODE)) {
-            for (int i = 0; i < bn_boxes; ++i)
-              tma_load_2d(b + i * kAtomBytes, &tmB, &full[stage], n0 + 64 * i, kb * kBK, pol);
+#pragma unroll
+            for (int i = 0; i < kBN / CG / 64; ++i)
+              load(b + i * kAtomBytes, &tmB, n0 + 64 * i, kb * kBK, pol_b);
           } else {
-            tma_load_2d(b, &tmB, &full[stage], kb * kBK, n0, pol);
+            load(b, &tmB, kb * kBK, n0, pol_b);
           }
-          issued[stage] = true;
-          parity[stage] = phase;
           if (++stage == kStages) stage = 0, phase ^= 1;
         }
       }
-      // never leave with copies in flight
-      for (int s = 0; s < kStages; ++s)
-        if (issued[s] && !mbar_wait(&full[s], parity[s], nullptr))
+      // Never leave with copies in flight: a stage is released once the MMAs that read its
+      // copies (of both CTAs) are done, so wait (bounded) for the release of every stage used.
+      for (int s = 0; s < kStages; ++s) {
+        const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
+        if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
           report(p.status, FQ_ERR_TIMEOUT);
+      }
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
-      const uint32_t idesc = umma_idesc_bf16(kBM, static_cast<uint32_t>(p.bn)) |
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = umma_idesc_bf16(CG * kBM, static_cast<uint32_t>(p.bn)) |
                              (a_mn_major(MODE) ? 1u << 15 : 0u) |
                              (b_mn_major(MODE) ? 1u << 16 : 0u);
       // 16 k per MMA: 32 bytes along a K-major row, or 16 rows of 128 bytes of an MN-major tile
@@ -249,103 +350,147 @@ __global__ void __launch_bounds__(kThreads, 1)
       constexpr uint64_t stepB = (b_mn_major(MODE) ? 2048 : 32) >> 4;
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
-      bool issued_any = false;
-      for (int u = cid; u < p.units && !*abort_flag; u += ncl) {
+      bool ok = true;
+      for (int u = cid; ok && u < p.units && !*abort_flag; u += ncl) {
         const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
-        bool ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
-        tc_fence_after_sync();
-        const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
-        for (int kb = k0; ok && kb < k1; ++kb) {
-          ok = mbar_wait(&full[stage], phase, abort_flag);
+        for (int ka = k0; ok && ka < k1;) {
+          const int ke = MODE == kLse ? min(k1, ka + kSegBlocks) : k1;
+          ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t sa = smem_u32(smem + oA + stage * kABytes);
-          const uint32_t sb = smem_u32(smem + oB + stage * kBBytes);
-          const uint64_t ad = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
-          const uint64_t bd = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
+          const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
+          for (int kb = ka; kb < ke; ++kb) {
+            ok = mbar_wait(&full[stage], phase, abort_flag);
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint32_t sa = smem_u32(smem + Lo::oA + stage * kABytes);
+            const uint32_t sb = smem_u32(smem + Lo::oB + stage * kBBytes);
+            const uint64_t ad = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
+            const uint64_t bd = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k)
-            umma_bf16(d, ad + k * stepA, bd + k * stepB, idesc, (kb > k0 || k > 0) ? 1u : 0u);
-          issued_any = true;
-          umma_commit(&empty[stage]);
-          if (++stage == kStages) stage = 0, phase ^= 1;
+            for (int k = 0; k < kBK / 16; ++k)
+              umma_cg<CG>(d, ad + k * stepA, bd + k * stepB, idesc,
+                          (kb > ka || k > 0) ? 1u : 0u);
+            umma_commit_cg<CG>(&empty[stage]);
+            if (++stage == kStages) stage = 0, phase ^= 1;
+          }
+          if (!ok) break;
+          umma_commit_cg<CG>(&tfull[buf]);
+          if (++buf == 2) buf = 0, acc_phase ^= 1;
+          ka = ke;
         }
-        if (!ok) {
-          report(p.status, FQ_ERR_TIMEOUT);
-          *abort_flag = 1;
-          break;
-        }
-        umma_commit(&tfull[buf]);
-        if (++buf == 2) buf = 0, acc_phase ^= 1;
       }
-      if (issued_any) {                          // every MMA done before the TMEM is released
-        umma_commit(mma_done);
-        if (!mbar_wait(mma_done, 0, nullptr)) report(p.status, FQ_ERR_TIMEOUT);
+      if (!ok) {
+        report(p.status, FQ_ERR_TIMEOUT);
+        *abort_flag = 1;
       }
     }
   } else {
     // ---------------------------------------------------------------- epilogue
-    const int quarter = warp & 3;
+    const int quarter = warp & 3;                 // TMEM lanes 32 * quarter .. + 31
+    const int half = (warp - 2) >> 2;
     const int r_in_tile = quarter * 32 + lane;
+    // this thread's columns [h0, h1) of a tile
+    const int hw = (p.bn / 2 + kChunk - 1) / kChunk * kChunk;
+    const int h0 = half * hw, h1 = half ? p.bn : hw;
     pdl_wait();
     int buf = 0;
     uint32_t acc_phase = 0;
+    auto wait_acc = [&]() {
+      // the warp leaves as one: the TMEM loads are warp-wide
+      if (__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
+        tc_fence_after_sync();
+        return true;
+      }
+      report(p.status, FQ_ERR_TIMEOUT);
+      *abort_flag = 1;
+      return false;
+    };
+    auto release_acc = [&]() {
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if (CG == 2) mbar_arrive_cluster(mapa(smem_u32(&tempty[buf]), 0));
+        else mbar_arrive(&tempty[buf]);
+      }
+      if (++buf == 2) buf = 0, acc_phase ^= 1;
+    };
     for (int u = cid; u < p.units; u += ncl) {
       const int nt = unit_nt(u);
-      const int row = unit_rt(u) * kBM + r_in_tile, n0 = nt * p.bn;
+      const int row = (unit_rt(u) * CG + rank) * kBM + r_in_tile;
+      const int n0 = nt * p.bn + h0;              // first column of this thread in the result
       const bool row_ok = row < p.R;
-      const int cols = min(p.bn, p.N - n0);      // valid columns of the tile
-      // the warp leaves as one: the TMEM loads below are warp-wide
-      if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
-        report(p.status, FQ_ERR_TIMEOUT);
-        *abort_flag = 1;
-        break;
-      }
-      tc_fence_after_sync();
-      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
-                             static_cast<uint32_t>(buf * kBN);
-      if (MODE == kLse || MODE == kDl) {
-        const int64_t lrow = row_ok ? row : 0;
-        EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, p.v0 + n0);
-        const float c2 = p.scale * kLog2e;
-        float m = -CUDART_INF_F, sum = 0.f;      // running maximum and sum, in units of log 2
-        float lse2 = 0.f, g = 0.f;
-        bool has = false;
-        if (MODE == kDl && row_ok) {
-          const int first = __ldcg(p.entry + lrow * p.E);
-          has = first >= 0 && first < p.V;
-          lse2 = __ldcg(p.lse + row) * kLog2e;
-          g = __ldcg(p.dloss + row) * p.gscale;
+      const int64_t lrow = row_ok ? row : 0;
+      const int cols = min(h1 - h0, p.N - n0);    // valid columns of this thread (may be <= 0)
+      const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + h0;
+      if constexpr (MODE == kLse) {
+        float acc[kHalf];
+#pragma unroll
+        for (int q = 0; q < kHalf; ++q) acc[q] = 0.f;
+        bool ok = true;
+        for (int ka = 0; ka < p.KB; ka += kSegBlocks) {
+          ok = wait_acc();
+          if (!ok) break;
+          const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
+#pragma unroll
+          for (int c = 0; c < kHalf; c += 16) {
+            float v[16];
+            tmem_ld16(t_row + c, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[c + q] += v[q];
+          }
+          release_acc();
         }
+        if (!ok) break;
+        EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, n0);
+        const float c2 = p.scale * kLog2e;
+        float m = -CUDART_INF_F, sum = 0.f;       // maximum and sum, in units of log 2
+#pragma unroll
+        for (int c = 0; c < kHalf; c += kChunk) {
+          while (w.next < n0 + min(c + kChunk, cols)) {
+            const int j = w.next - (n0 + c);
+            float z = 0.f;
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) z = q == j ? acc[c + q] : z;
+            p.zt[lrow * p.E + w.k] = z * p.scale;
+            w.step();
+          }
+#pragma unroll
+          for (int q = 0; q < kChunk; ++q) {
+            acc[c + q] = c + q < cols ? acc[c + q] * c2 : -CUDART_INF_F;
+            m = fmaxf(m, acc[c + q]);
+          }
+        }
+        const float ref = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 8) {
+          float s = 0.f;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) s += ex2(acc[c + q] - ref);
+          sum += s;
+        }
+        if (row_ok) p.part[(static_cast<int64_t>(nt) * 2 + half) * p.R + row] = make_float2(m, sum);
+      } else {
+        if (!wait_acc()) break;
+        const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
+        if (MODE == kDl) {
+          EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, p.v0 + n0);
+          const float c2 = p.scale * kLog2e;
+          float lse2 = 0.f, g = 0.f;
+          bool has = false;
+          if (row_ok) {
+            const int first = __ldcg(p.entry + lrow * p.E);
+            has = first >= 0 && first < p.V;
+            lse2 = __ldcg(p.lse + row) * kLog2e;
+            g = __ldcg(p.dloss + row) * p.gscale;
+          }
 #pragma unroll 1
-        for (int c = 0; c < cols; c += kChunk) {
-          float v[kChunk];
-          __syncwarp();
-          tmem_ld32(t_row + c, v);
-          tmem_wait_ld();
-          if (MODE == kLse) {
-            while (w.next < p.v0 + n0 + c + kChunk && w.next < p.v0 + n0 + cols) {
-              const int j = w.next - (p.v0 + n0 + c);
-              float z = 0.f;
-#pragma unroll
-              for (int q = 0; q < kChunk; ++q) z = q == j ? v[q] : z;
-              p.zt[lrow * p.E + w.k] = z * p.scale;
-              w.step();
-            }
-            float cm = -CUDART_INF_F;
-#pragma unroll
-            for (int q = 0; q < kChunk; ++q) {
-              v[q] = c + q < cols ? v[q] * c2 : -CUDART_INF_F;
-              cm = fmaxf(cm, v[q]);
-            }
-            const float mn = fmaxf(m, cm);
-            const float ref = mn == -CUDART_INF_F ? 0.f : mn;
-            float s = 0.f;
-#pragma unroll
-            for (int q = 0; q < kChunk; ++q) s += ex2(v[q] - ref);
-            sum = fmaf(sum, ex2(m - ref), s);
-            m = mn;
-          } else {
+          for (int c = 0; c < cols; c += kChunk) {
+            float v[kChunk];
+            __syncwarp();
+            tmem_ld32(t_row + c, v);
+            tmem_wait_ld();
 #pragma unroll
             for (int q = 0; q < kChunk; ++q) v[q] = ex2(fmaf(v[q], c2, -lse2));
             while (w.next < p.v0 + n0 + c + kChunk) {
@@ -359,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint4* dst = reinterpret_cast<uint4*>(p.out + row * p.ldo + n0 + c);
 #pragma unroll
               for (int q = 0; q < kChunk; q += 8) {
-                if (c + q >= p.bn) break;        // the next tile's columns
+                if (c + q >= h1 - h0) break;       // the next tile's columns
                 uint4 o;
                 o.x = has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u;
                 o.y = has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u;
@@ -369,57 +514,57 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
           }
-        }
-        if (MODE == kLse && row_ok)
-          p.part[static_cast<int64_t>(nt) * p.R + row] = make_float2(m, sum);
-      } else {
-        // result rows; N is a multiple of 8
-        float* o32 = p.out32 ? p.out32 + (static_cast<int64_t>(unit_ks(u)) * p.R + row) * p.N + n0
-                             : nullptr;
-        __nv_bfloat16* o16 = p.out + static_cast<int64_t>(row) * p.ldo + n0;
+        } else {
+          // result rows; N is a multiple of 8
+          const int ks = unit_ks(u);
+          float* o32 = p.out32 ? p.out32 + (static_cast<int64_t>(ks) * p.R + row) * p.N + n0
+                               : nullptr;
+          __nv_bfloat16* o16 = p.out + static_cast<int64_t>(row) * p.ldo + n0;
 #pragma unroll 1
-        for (int c = 0; c < cols; c += kChunk) {
-          float v[kChunk];
-          __syncwarp();
-          tmem_ld32(t_row + c, v);
-          tmem_wait_ld();
-          if (!row_ok) continue;
+          for (int c = 0; c < cols; c += kChunk) {
+            float v[kChunk];
+            __syncwarp();
+            tmem_ld32(t_row + c, v);
+            tmem_wait_ld();
+            if (!row_ok) continue;
 #pragma unroll
-          for (int q = 0; q < kChunk; q += 8) {
-            if (c + q >= cols) break;
-            if (MODE == kDx && o32) {
+            for (int q = 0; q < kChunk; q += 8) {
+              if (c + q >= cols) break;
+              if (MODE == kDx && o32) {
 #pragma unroll
-              for (int h = 0; h < 8; h += 4) {
-                float4* dst = reinterpret_cast<float4*>(o32 + c + q + h);
-                float4 o = make_float4(v[q + h], v[q + h + 1], v[q + h + 2], v[q + h + 3]);
-                if (unit_ks(u) < p.filled) {
-                  const float4 old = *dst;
-                  o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+                for (int h = 0; h < 8; h += 4) {
+                  float4* dst = reinterpret_cast<float4*>(o32 + c + q + h);
+                  float4 o = make_float4(v[q + h], v[q + h + 1], v[q + h + 2], v[q + h + 3]);
+                  if (ks < p.filled) {
+                    const float4 old = *dst;
+                    o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+                  }
+                  *dst = o;
                 }
-                *dst = o;
+              } else {
+                uint4 o;
+                o.x = pack_bf16(v[q], v[q + 1]);
+                o.y = pack_bf16(v[q + 2], v[q + 3]);
+                o.z = pack_bf16(v[q + 4], v[q + 5]);
+                o.w = pack_bf16(v[q + 6], v[q + 7]);
+                *reinterpret_cast<uint4*>(o16 + c + q) = o;
               }
-            } else {
-              uint4 o;
-              o.x = pack_bf16(v[q], v[q + 1]);
-              o.y = pack_bf16(v[q + 2], v[q + 3]);
-              o.z = pack_bf16(v[q + 4], v[q + 5]);
-              o.w = pack_bf16(v[q + 6], v[q + 7]);
-              *reinterpret_cast<uint4*>(o16 + c + q) = o;
             }
           }
         }
+        release_acc();
       }
-      tc_fence_before_sync();
-      mbar_arrive(&tempty[buf]);
-      if (++buf == 2) buf = 0, acc_phase ^= 1;
     }
   }
 
+  // Every MMA has completed (each accumulator was waited for) and every stage was released
+  // before the TMEM goes and the pair parts.
   tc_fence_before_sync();
   __syncthreads();
+  if (CG == 2) cluster_sync();
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, kTmemCols);
+    tmem_dealloc_cg<CG>(tmem_base, kTmemCols);
   }
 }
 
@@ -629,26 +774,76 @@ cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t sm
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int MODE>
-fq_status launch_gemm(const CUtensorMap& a, const CUtensorMap& b, GemmArgs& g, int sms,
-                      cudaStream_t s) {
+// CTA pairs that fit the device at once (its SMs in pairs, where the launch limits allow).
+template <int MODE, int CG>
+fq_status prepare_gemm(int& clusters) {
   static std::mutex mu;
-  static std::map<int, bool> done;
-  {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!done[dev]) {
-      if (cudaFuncSetAttribute(head_gemm_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               kSmemBytes) != cudaSuccess)
+  static std::map<int, int> fit;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(mu);
+  auto it = fit.find(dev);
+  if (it == fit.end()) {
+    if (cudaFuncSetAttribute(head_gemm_kernel<MODE, CG>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             Lay<CG>::kBytes) != cudaSuccess)
+      return FQ_ERR_CUDA;
+    int n = sm_count();
+    if (CG == 2) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3(static_cast<unsigned>(n / 2 * 2));
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = Lay<CG>::kBytes;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 2;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int most = 0;
+      if (cudaOccupancyMaxActiveClusters(&most, head_gemm_kernel<MODE, CG>, &cfg) != cudaSuccess ||
+          most < 1)
         return FQ_ERR_CUDA;
-      done[dev] = true;
+      n = std::min(n / 2, most);
     }
+    it = fit.emplace(dev, n).first;
   }
-  return launch(head_gemm_kernel<MODE>, std::min(g.units, sms), kThreads, kSmemBytes, s, a, b,
-                g) == cudaSuccess
-             ? FQ_OK
-             : FQ_ERR_CUDA;
+  clusters = it->second;
+  return FQ_OK;
+}
+
+template <int MODE, int CG>
+fq_status launch_gemm_cg(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g,
+                         cudaStream_t s) {
+  int clusters = 0;
+  if (const fq_status st = prepare_gemm<MODE, CG>(clusters)) return st;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min(g.units, clusters) * CG));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Lay<CG>::kBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CG == 2 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, CG>, a, b, g) == cudaSuccess ? FQ_OK
+                                                                                      : FQ_ERR_CUDA;
+}
+
+// CTAs per tile: a pair where the result has more than one CTA's rows.
+int group_for(int R) { return R > kBM ? 2 : 1; }
+
+template <int MODE>
+fq_status launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g,
+                      cudaStream_t s) {
+  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(a, b, g, s)
+                             : launch_gemm_cg<MODE, 1>(a, b, g, s);
 }
 
 void plan(GemmArgs& g, int R, int N, int K, int bn, int splits) {
@@ -656,7 +851,10 @@ void plan(GemmArgs& g, int R, int N, int K, int bn, int splits) {
   g.N = N;
   g.K = K;
   g.bn = bn;
-  g.RT = static_cast<int>(ceil_div(R, kBM));
+  // rows of the accumulator beyond R are never read, so what A's stage holds there (earlier
+  // copies, or nothing yet) does not matter
+  g.a_rows = static_cast<int>(std::min<int64_t>(kBM, round_up(R, 8)));
+  g.RT = static_cast<int>(ceil_div(R, kBM * group_for(R)));
   g.NT = static_cast<int>(ceil_div(N, bn));
   g.KB = static_cast<int>(ceil_div(K, kBK));
   g.kbs = static_cast<int>(ceil_div(g.KB, splits));
@@ -664,24 +862,26 @@ void plan(GemmArgs& g, int R, int N, int K, int bn, int splits) {
   g.units = g.RT * g.NT * g.KS;
 }
 
-// Columns per tile of the logit products: the width whose rounds of tiles over the SMs take the
-// least time (a tile's time is proportional to its width), the widest of equals.
+// Columns per tile of the logit products.  A tile's time hardly depends on its width (19.4 us at
+// 128 columns and 23.0 us at 256 for d = 4096, CG = 2), so tiles are as wide as they go, unless
+// all of them fit the SMs (or pairs) at once: then they are as narrow as still does.
 int pick_bn(int R, int N, int sms) {
-  const int64_t RT = ceil_div(R, kBM);
-  int best = kBN;
-  int64_t cost = -1;
-  for (int bn = kBN; bn >= 128; bn -= 16) {
-    const int64_t c = ceil_div(RT * ceil_div(N, bn), sms) * bn;
-    if (cost < 0 || c < cost) cost = c, best = bn;
-  }
-  return best;
+  const int cg = group_for(R);
+  const int64_t RT = ceil_div(R, kBM * cg), room = std::min(sms, kMaxSms) / cg;
+  int bn = kBN;
+  while (bn > kMinBn && RT * ceil_div(N, bn - 16 * cg) <= room) bn -= 16 * cg;
+  return bn;
 }
 
-constexpr int kMinBn = 128;
+// Most column tiles of the logit products on any device.
+int64_t most_tiles(int R, int N) {
+  const int cg = group_for(R);
+  return std::max<int64_t>(ceil_div(N, kBN), kMaxSms / cg / ceil_div(R, kBM * cg));
+}
+
 constexpr int64_t kPieceBytes = 128ll << 20;    // ds of one piece of the vocabulary
 constexpr int kMinPiece = 2048;
 constexpr int kMaxSlots = 16;                   // fp32 slots of a dx split over the vocabulary
-constexpr int kMaxSms = 256;                    // bound on the SM count used for planning
 
 // Vocabulary entries per piece: as many as kPieceBytes of ds hold (at least kMinPiece), in
 // pieces of equal size rounded up to 256.
@@ -693,7 +893,7 @@ int piece_width(int M, int V) {
 
 // Ways the contraction of dx over a piece is split, so that few tiles still fill the SMs.
 int dx_splits(int M, int d, int Vc, int sms) {
-  const int64_t tiles = ceil_div(M, kBM) * ceil_div(d, kBN);
+  const int64_t tiles = ceil_div(M, kBM * group_for(M)) * group_for(M) * ceil_div(d, kBN);
   const int64_t KB = ceil_div(Vc, kBK);
   return static_cast<int>(std::max<int64_t>(
       1, std::min<int64_t>({kMaxSlots, std::min(sms, kMaxSms) / tiles, KB / 8})));
@@ -717,7 +917,7 @@ Ws ws_layout(int M, int d, int V, int K, bool grad) {
   L.plogp = take(static_cast<size_t>(M) * 4);
   if (!grad) {
     L.zt = take(mk);
-    L.part = take(static_cast<size_t>(ceil_div(V, kMinBn)) * M * 8);
+    L.part = take(static_cast<size_t>(most_tiles(M, V)) * 2 * M * 8);
   } else {
     const int P = piece_width(M, V);
     L.xc = take(static_cast<size_t>(M) * d * 2);
@@ -797,7 +997,8 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   GemmArgs g{};
   plan(g, M, V, d, pick_bn(M, V, sms), 1);
   CUtensorMap mx, mw;
-  if (!make_tmap(&mx, x, M, d, d, kBM) || !make_tmap(&mw, W, V, d, d, g.bn)) return FQ_ERR_CUDA;
+  if (!make_tmap(&mx, x, M, d, d, g.a_rows) || !make_tmap(&mw, W, V, d, d, g.bn / group_for(M)))
+    return FQ_ERR_CUDA;
   const float* plogp = nullptr;
   if (const fq_status st = launch_entries(t, M, V, L, ws, g.entry, g.prob, plogp, s)) return st;
   g.status = reinterpret_cast<int32_t*>(ws);
@@ -807,9 +1008,9 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   g.V = V;
   g.part = reinterpret_cast<float2*>(ws + L.part);
   g.zt = reinterpret_cast<float*>(ws + L.zt);
-  if (const fq_status st = launch_gemm<kLse>(mx, mw, g, sms, s)) return st;
+  if (const fq_status st = launch_gemm<kLse>(mx, mw, g, s)) return st;
   return launch(head_join_kernel, ceil_div(M, kJoinWarps), 32 * kJoinWarps, 0, s,
-                static_cast<const float2*>(g.part), g.NT, M, V, t.given, g.entry, g.prob,
+                static_cast<const float2*>(g.part), 2 * g.NT, M, V, t.given, g.entry, g.prob,
                 static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, loss,
                 lse, g.status) == cudaSuccess
              ? FQ_OK
@@ -855,7 +1056,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     {
       GemmArgs g{};
       plan(g, M, Vc, d, pick_bn(M, Vc, sms), 1);
-      if (!make_tmap(&mx, xc, M, d, d, kBM) || !make_tmap(&mw, Wq, Vc, d, d, g.bn))
+      if (!make_tmap(&mx, xc, M, d, d, g.a_rows) || !make_tmap(&mw, Wq, Vc, d, d, g.bn / group_for(M)))
         return FQ_ERR_CUDA;
       g.status = status;
       g.scale = 1.f / t.tau;
@@ -869,13 +1070,13 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.gscale = t.logit ? t.tau : 1.f;
       g.out = ds;
       g.ldo = ldds;
-      if (const fq_status st = launch_gemm<kDl>(mx, mw, g, sms, s)) return st;
+      if (const fq_status st = launch_gemm<kDl>(mx, mw, g, s)) return st;
     }
     CUtensorMap ma, mb;
     if (dx) {
       GemmArgs g{};
       plan(g, M, d, Vc, kBN, splits);
-      if (!make_tmap(&ma, ds, M, Vc, ldds, kBM) || !make_tmap(&mb, Wq, Vc, d, d, kBK))
+      if (!make_tmap(&ma, ds, M, Vc, ldds, g.a_rows) || !make_tmap(&mb, Wq, Vc, d, d, kBK))
         return FQ_ERR_CUDA;
       g.status = status;
       g.out = static_cast<__nv_bfloat16*>(dx);
@@ -883,7 +1084,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.out32 = direct ? nullptr : slots;
       g.filled = used;
       used = std::max(used, g.KS);
-      if (const fq_status st = launch_gemm<kDx>(ma, mb, g, sms, s)) return st;
+      if (const fq_status st = launch_gemm<kDx>(ma, mb, g, s)) return st;
     }
     if (dW) {
       GemmArgs g{};
@@ -893,7 +1094,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.status = status;
       g.out = static_cast<__nv_bfloat16*>(dW) + static_cast<int64_t>(v0) * d;
       g.ldo = d;
-      if (const fq_status st = launch_gemm<kDw>(ma, mb, g, sms, s)) return st;
+      if (const fq_status st = launch_gemm<kDw>(ma, mb, g, s)) return st;
     }
   }
   if (dx && !direct) {
