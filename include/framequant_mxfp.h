@@ -1,0 +1,75 @@
+/*
+ * libframequant, microscaled 4-bit floating point (MXFP4 of the OCP Microscaling Formats
+ * specification): the 4-bit format that the tensor cores multiply directly, next to the 2-bit
+ * frame coefficients of framequant.h.
+ *
+ * A row of 32 k values is k blocks of 32.  A block with largest magnitude a has the scale
+ * 2^e, e = max(floor(log2 a) - 2, -127), and each value v the E2M1 code of v / 2^e: one of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign, to nearest with ties to the even code, saturating at 6.
+ * A block that holds an infinity or a NaN has the scale NaN: all its values read back as NaN, and
+ * so does every result that it takes part in.  4.25 bits per value.
+ *
+ *   linear   y = Q(x) Q(W)^T,  both operands quantised, products and block scales exact, sums
+ *            in fp32 on the tensor cores, y rounded to bf16 once
+ *
+ * Conventions are those of framequant.h (device pointers, 16-byte alignment, asynchronous on
+ * `stream`, validation before any launch, no allocation by the library).
+ */
+#ifndef FRAMEQUANT_MXFP_H_
+#define FRAMEQUANT_MXFP_H_
+
+#include "framequant.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* A quantised matrix: descriptor and its caller-owned device buffers.
+ *   codes   fq_mxfp_codes_bytes: row-major, cols / 2 bytes a row, the even column in the low
+ *           four bits (bit 3 is the sign)
+ *   scales  fq_mxfp_scales_bytes: e + 127 as one byte a block (255: NaN), in the order in which
+ *           the tensor cores take them: 512-byte tiles of 128 rows x 4 blocks, byte
+ *           16 (r % 32) + 4 (r / 32 % 4) + b of a tile for row r and block b, tiles of a row
+ *           group along the columns, an even number of them; what lies beyond the matrix is 0 */
+typedef struct {
+  uint8_t* codes;
+  uint8_t* scales;
+  int32_t rows, cols;
+} fq_mxfp;
+
+/* Bytes of the two buffers; 0 for invalid sizes (rows < 1, cols not a positive multiple of 32). */
+size_t fq_mxfp_codes_bytes(int rows, int cols);
+size_t fq_mxfp_scales_bytes(int rows, int cols);
+
+/* Quantise x (device bf16 rows x cols) into q, whose rows and cols are those given.
+ * Errors: FQ_ERR_INVALID_ARG (a null pointer, rows < 1, cols not a positive multiple of 32, q of
+ * other sizes), FQ_ERR_ALIGNMENT, FQ_ERR_UNSUPPORTED (device not compute capability 10.3),
+ * FQ_ERR_CUDA. */
+fq_status fq_mxfp_quantize(const void* x, int rows, int cols, const fq_mxfp* q,
+                           fq_stream_t stream);
+
+/* The values that q stands for, exact in bf16: y device bf16 rows x cols.  Errors as above. */
+fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream);
+
+/* y = X W^T for quantised X (M x d) and W (d_out x d), y device bf16 M x d_out; d_out of any
+ * size.  status: device int32 for fq_check (cleared by the call), or NULL.
+ * Errors as above (FQ_ERR_INVALID_ARG also where X and W differ in cols). */
+fq_status fq_mxfp_product(const fq_mxfp* X, const fq_mxfp* W, void* y, int32_t* status,
+                          fq_stream_t stream);
+
+/* Workspace bytes of fq_mxfp_linear (the quantised x); 0 for invalid sizes. */
+size_t fq_mxfp_workspace_bytes(int M, int d_in, int d_out);
+
+/* y = Q(x) W^T for M tokens: fq_mxfp_quantize of x into the workspace, then the product.
+ *   x   device bf16 M x d_in;  W  quantised d_out x d_in;  y  device bf16 M x d_out
+ *   ws  device workspace of fq_mxfp_workspace_bytes(M, d_in, d_out) bytes, 256-byte aligned; it
+ *       need not be cleared, and its head is the status word of fq_check
+ * Errors: as fq_mxfp_product, and FQ_ERR_WORKSPACE. */
+fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void* y, void* ws,
+                         size_t ws_bytes, fq_stream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* FRAMEQUANT_MXFP_H_ */

@@ -28,6 +28,8 @@ __all__ = [
     "fq_linear_forward_implicit_group", "ImplicitLayer", "fq_frame_tiles_bytes", "fq_frame_tile",
     "fq_head_workspace_bytes", "fq_head_grad_workspace_bytes", "fq_cross_entropy",
     "fq_cross_entropy_grad", "fq_distill", "fq_distill_grad", "FQ_DISTILL_MAX_K",
+    "Mxfp", "fq_mxfp_alloc", "fq_mxfp_codes_bytes", "fq_mxfp_scales_bytes", "fq_mxfp_quantize",
+    "fq_mxfp_dequantize", "fq_mxfp_product", "fq_mxfp_workspace_bytes", "fq_mxfp_linear",
 ]
 FQ_MAX_GROUP = 4
 FQ_STATIC_SCRATCH_BYTES = 16 << 20
@@ -56,7 +58,9 @@ EXPORTED = ("fq_packed_words", "fq_pack", "fq_workspace_bytes", "fq_linear_forwa
             "fq_quantize_gptq", "fq_implicit_group_workspace_bytes",
             "fq_linear_forward_implicit_group", "fq_frame_tiles_bytes", "fq_frame_tile",
             "fq_head_workspace_bytes", "fq_head_grad_workspace_bytes", "fq_cross_entropy",
-            "fq_cross_entropy_grad", "fq_distill", "fq_distill_grad")
+            "fq_cross_entropy_grad", "fq_distill", "fq_distill_grad", "fq_mxfp_codes_bytes",
+            "fq_mxfp_scales_bytes", "fq_mxfp_quantize", "fq_mxfp_dequantize", "fq_mxfp_product",
+            "fq_mxfp_workspace_bytes", "fq_mxfp_linear")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -109,6 +113,11 @@ class _Frame(ctypes.Structure):
                 ("ana_idx", ctypes.c_void_p), ("ana_count", ctypes.c_int32),
                 ("syn_tiles", ctypes.c_void_p), ("syn_idx", ctypes.c_void_p),
                 ("syn_count", ctypes.c_int32)]
+
+
+class _Mxfp(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("rows", ctypes.c_int32), ("cols", ctypes.c_int32)]
 
 
 _lib = None
@@ -243,6 +252,20 @@ def lib() -> ctypes.CDLL:
         L.fq_distill_grad.restype = ci
         L.fq_distill_grad.argtypes = [vp, ci, ci, vp, ci, vp, vp, ci, ctypes.c_float, vp, vp, vp,
                                       vp, vp, sz, vp]
+        qp = ctypes.POINTER(_Mxfp)
+        for name in ("fq_mxfp_codes_bytes", "fq_mxfp_scales_bytes"):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [ci] * 2
+        L.fq_mxfp_workspace_bytes.restype = sz
+        L.fq_mxfp_workspace_bytes.argtypes = [ci] * 3
+        L.fq_mxfp_quantize.restype = ci
+        L.fq_mxfp_quantize.argtypes = [vp, ci, ci, qp, vp]
+        L.fq_mxfp_dequantize.restype = ci
+        L.fq_mxfp_dequantize.argtypes = [qp, vp, vp]
+        L.fq_mxfp_product.restype = ci
+        L.fq_mxfp_product.argtypes = [qp, qp, vp, vp, vp]
+        L.fq_mxfp_linear.restype = ci
+        L.fq_mxfp_linear.argtypes = [vp, ci, ci, qp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -666,3 +689,71 @@ def fq_distill_grad(x, M: int, d: int, W, V: int, index, logit, K: int, tau: flo
         _arr(index, _I32, M * K, "index"), _arr(logit, _F32, M * K, "logit"), K, tau,
         _arr(lse, _F32, M, "lse"), _arr(dloss, _F32, M, "dloss"), _arr(dx, _BF, M * d, "dx"),
         _arr(dW, _BF, V * d, "dW"), _ptr(ws), ws_bytes, _stream(stream)), "fq_distill_grad")
+
+
+# ------------------------------------------------------- microscaled 4-bit floating point
+@dataclass
+class Mxfp:
+    """A microscaled 4-bit matrix (include/framequant_mxfp.h): device tensors of codes and
+    scales (uint8) and the sizes.  fq_mxfp_alloc makes one, fq_mxfp_quantize fills it."""
+    codes: object
+    scales: object
+    rows: int
+    cols: int
+
+    def _c(self) -> _Mxfp:
+        return _Mxfp(_arr(self.codes, "torch.uint8", self.rows * (self.cols // 2), "codes"),
+                     _arr(self.scales, "torch.uint8",
+                          fq_mxfp_scales_bytes(self.rows, self.cols), "scales"),
+                     self.rows, self.cols)
+
+
+def fq_mxfp_codes_bytes(rows: int, cols: int) -> int:
+    return lib().fq_mxfp_codes_bytes(rows, cols)
+
+
+def fq_mxfp_scales_bytes(rows: int, cols: int) -> int:
+    return lib().fq_mxfp_scales_bytes(rows, cols)
+
+
+def fq_mxfp_alloc(rows: int, cols: int, device=None) -> Mxfp:
+    """Device buffers of a rows x cols matrix, allocated with torch."""
+    import torch
+    nc, ns = fq_mxfp_codes_bytes(rows, cols), fq_mxfp_scales_bytes(rows, cols)
+    if nc == 0 or ns == 0:
+        raise FrameQuantError(1, "fq_mxfp_alloc")
+    dev = device or "cuda"
+    return Mxfp(torch.empty(nc, dtype=torch.uint8, device=dev),
+                torch.empty(ns, dtype=torch.uint8, device=dev), rows, cols)
+
+
+def fq_mxfp_quantize(x, rows: int, cols: int, q: Mxfp, stream=None) -> None:
+    c = q._c()
+    _ok(lib().fq_mxfp_quantize(_arr(x, _BF, rows * cols, "x"), rows, cols, ctypes.byref(c),
+                               _stream(stream)), "fq_mxfp_quantize")
+
+
+def fq_mxfp_dequantize(q: Mxfp, y, stream=None) -> None:
+    c = q._c()
+    _ok(lib().fq_mxfp_dequantize(ctypes.byref(c), _arr(y, _BF, q.rows * q.cols, "y"),
+                                 _stream(stream)), "fq_mxfp_dequantize")
+
+
+def fq_mxfp_product(X: Mxfp, W: Mxfp, y, status=None, stream=None) -> None:
+    """y = X W^T (bf16 X.rows x W.rows) on the block-scaled tensor cores."""
+    cx, cw = X._c(), W._c()
+    _ok(lib().fq_mxfp_product(ctypes.byref(cx), ctypes.byref(cw),
+                              _arr(y, _BF, X.rows * W.rows, "y"), _arr(status, _I32, 1, "status"),
+                              _stream(stream)), "fq_mxfp_product")
+
+
+def fq_mxfp_workspace_bytes(M: int, d_in: int, d_out: int) -> int:
+    return lib().fq_mxfp_workspace_bytes(M, d_in, d_out)
+
+
+def fq_mxfp_linear(x, M: int, d_in: int, W: Mxfp, y, ws, ws_bytes: int, stream=None) -> None:
+    """y = Q(x) W^T for M tokens, x quantised on the way (include/framequant_mxfp.h)."""
+    c = W._c()
+    _ok(lib().fq_mxfp_linear(_arr(x, _BF, M * d_in, "x"), M, d_in, ctypes.byref(c),
+                             _arr(y, _BF, M * W.rows, "y"), _ptr(ws), ws_bytes, _stream(stream)),
+        "fq_mxfp_linear")

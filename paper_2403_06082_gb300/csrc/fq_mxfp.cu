@@ -1,0 +1,671 @@
+// Microscaled 4-bit floating point (include/framequant_mxfp.h): quantisation, and the product of
+// two quantised matrices on the block-scaled tensor cores (kind::mxf4: E2M1 operands, one
+// power-of-two scale per row and 32 k, fp32 accumulation).
+//
+// Product: y[t][i] = sum_k W[i][k] X[t][k].  A tile is 128 rows of W (the accumulator's rows) x
+// bn <= 192 tokens.  Codes arrive by TMA, 256 k (128 bytes) a stage under the 128-byte swizzle;
+// scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage, and go
+// through shared memory into TMEM (tcgen05.cp) ahead of the stage's four MMAs of 64 k.  Of the
+// 512 TMEM columns two accumulators take 2 x 192 and every stage has 24 of its own for scales,
+// so no copy waits for an MMA other than its stage's last user.
+//
+// Few tokens read W once at memory speed; the tiles are then too few for the SMs, so a cluster of
+// KS CTAs splits the k range of one tile and adds the parts up, in rank order, through
+// distributed shared memory.
+//
+// Warp roles: warp 0 producer (one lane), warp 1 TMEM owner + MMA issuer (one lane), warps 2-9
+// epilogue (thread = accumulator row, half of the tokens).
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <map>
+#include <mutex>
+
+#include "fq_device.cuh"
+#include "fq_internal.h"
+#include "framequant_mxfp.h"
+
+namespace fq {
+namespace {
+
+constexpr int kBM = 128;                        // rows of W per tile
+constexpr int kBN = 192;                        // tokens per tile, at most
+constexpr int kKStage = 256;                    // k per stage: 128 bytes of codes a row
+constexpr int kABytes = kBM * kKStage / 2;
+constexpr int kBBytes = kBN * kKStage / 2;
+constexpr int kSfBytes = 1024;                  // scales of 128 rows x 256 k
+constexpr int kStageSf = 3 * kSfBytes;          // W's, and up to two row groups of X's
+constexpr int kStages = 5;
+constexpr int kThreads = 320;
+constexpr int kTmemCols = 512;
+constexpr int kSfCol = 2 * kBN;                 // TMEM columns of the scales, 24 a stage
+constexpr int kSfCols = 24;
+static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "tensor memory");
+
+constexpr int oA = 0;
+constexpr int oB = oA + kStages * kABytes;
+constexpr int oSf = oB + kStages * kBBytes;
+constexpr int oBar = oSf + kStages * kStageSf;
+constexpr int oMisc = oBar + (2 * kStages + 4) * 8;
+constexpr int kSmemBytes = oMisc + 16 + 1024;   // + alignment slack
+static_assert(kSmemBytes <= 227 * 1024, "shared memory");
+static_assert(kBN * kBM * 4 <= oBar, "a tile's fp32 part fits the stages");
+
+struct ProdArgs {
+  int R, M;                   // rows of W, tokens
+  int bn;                     // tokens per tile
+  int RT, TT, KB, KS, kbs;    // tiles of W, of tokens, stages of k, and the split of k
+  int units;                  // tiles (KS == 1)
+  const uint8_t* sw;          // scales of W, of X: 1 KiB per row group and stage
+  const uint8_t* sx;
+  int xgroups;                // row groups of X's scales
+  int early_w;                // W does not depend on the kernel before this one
+  __nv_bfloat16* y;
+  int32_t* status;
+};
+
+// Shared-memory descriptor of 32 x 128-bit scale rows without swizzle: 8 rows of 16 bytes are
+// 128 contiguous bytes, and so are the next 8 (stride byte offset 128).
+__device__ __forceinline__ uint64_t sf_desc(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF);
+  d |= static_cast<uint64_t>(1) << 16;
+  d |= static_cast<uint64_t>(128 >> 4) << 32;
+  d |= static_cast<uint64_t>(1) << 46;
+  return d;
+}
+
+// 512 bytes of scales (128 rows x 4) -> 4 TMEM columns, in all four lane quarters.
+__device__ __forceinline__ void sf_copy(uint32_t tmem, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc)
+               : "memory");
+}
+
+// Instruction descriptor, kind::mxf4: E2M1 A and B (1), power-of-two scales (bit 23), fp32
+// accumulator, both K-major, 128 x N; sf: which pair of the scale words' four bytes (0 or 2).
+__device__ __forceinline__ uint32_t idesc_mxf4(uint32_t N, uint32_t sf) {
+  return (sf << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) |
+         ((static_cast<uint32_t>(kBM) >> 4) << 24) | (sf << 29);
+}
+
+__device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
+                                          uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
+      "[%5], p;\n\t}" ::"r"(tmem_d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+    mxfp_product_kernel(const __grid_constant__ CUtensorMap tmW,
+                        const __grid_constant__ CUtensorMap tmX, const ProdArgs p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);
+  uint64_t* empty = full + kStages;
+  uint64_t* tfull = empty + kStages;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + oMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // SPLIT: one tile per cluster, its k range over the ranks; else tiles in turn
+  const int rank = SPLIT ? static_cast<int>(cluster_ctarank()) : 0;
+  const int first = SPLIT ? static_cast<int>(blockIdx.x) / p.KS : static_cast<int>(blockIdx.x);
+  const int step = SPLIT ? p.units : static_cast<int>(gridDim.x);
+  const int k0 = SPLIT ? min(p.KB, rank * p.kbs) : 0;
+  const int k1 = SPLIT ? min(p.KB, k0 + p.kbs) : p.KB;
+  // tile u = row tile * TT + token tile: the CTAs of a wave share W's tiles
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&tfull[b], 1);
+      mbar_init(&tempty[b], 8);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmW);
+    prefetch_tmap(&tmX);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_launch_dependents();
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- producer
+    if (lane == 0) {
+      const uint64_t pol_x = policy_evict_last();
+      const uint64_t pol_w = p.TT == 1 ? policy_evict_first() : pol_x;
+      auto load_w = [&](int st, int rt, int kb) {
+        tma_load_2d(smem + oA + st * kABytes, &tmW, &full[st], kb * (kKStage / 2), rt * kBM,
+                    pol_w);
+        bulk_load(smem + oSf + st * kStageSf, p.sw + (static_cast<int64_t>(rt) * p.KB + kb) * kSfBytes,
+                  kSfBytes, &full[st], pol_w);
+      };
+      auto load_x = [&](int st, int n0, int groups, int kb) {
+        tma_load_2d(smem + oB + st * kBBytes, &tmX, &full[st], kb * (kKStage / 2), n0, pol_x);
+        for (int g = 0; g < groups; ++g)
+          bulk_load(smem + oSf + st * kStageSf + (1 + g) * kSfBytes,
+                    p.sx + (static_cast<int64_t>(n0 / 128 + g) * p.KB + kb) * kSfBytes, kSfBytes,
+                    &full[st], pol_x);
+      };
+      // row groups of X's scales that a tile touches and that exist
+      auto groups_of = [&](int n0) {
+        return min(p.xgroups, (n0 + p.bn + 127) / 128) - n0 / 128;
+      };
+      auto bytes_of = [&](int groups) {
+        return static_cast<uint32_t>(kABytes + p.bn * (kKStage / 2) + (1 + groups) * kSfBytes);
+      };
+      int pre = 0;
+      if (p.early_w && first < p.units) {
+        pre = min(kStages, k1 - k0);
+        for (int i = 0; i < pre; ++i) {
+          mbar_arrive_expect_tx(&full[i], bytes_of(groups_of(first % p.TT * p.bn)));
+          load_w(i, first / p.TT, k0 + i);
+        }
+      }
+      pdl_wait();
+      if (p.status && blockIdx.x == 0) *p.status = 0;
+      int stage = 0;
+      uint32_t phase = 0;
+      int64_t it = 0;
+      for (int u = first; u < p.units && !*abort_flag; u += step) {
+        const int rt = u / p.TT, n0 = u % p.TT * p.bn, groups = groups_of(n0);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          if (it >= pre) {
+            if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
+              report(p.status, FQ_ERR_TIMEOUT);
+              *abort_flag = 1;
+              break;
+            }
+            mbar_arrive_expect_tx(&full[stage], bytes_of(groups));
+            load_w(stage, rt, kb);
+          }
+          load_x(stage, n0, groups, kb);
+          if (++stage == kStages) stage = 0, phase ^= 1;
+        }
+      }
+      // never leave with copies in flight: wait (bounded) for the release of every stage used
+      for (int s = 0; s < kStages; ++s) {
+        const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
+        if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
+          report(p.status, FQ_ERR_TIMEOUT);
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      const uint32_t id0 = idesc_mxf4(static_cast<uint32_t>(p.bn), 0);
+      const uint32_t id2 = idesc_mxf4(static_cast<uint32_t>(p.bn), 2);
+      int stage = 0, buf = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      for (int u = first; ok && k0 < k1 && u < p.units && !*abort_flag; u += step) {
+        const int n0 = u % p.TT * p.bn;
+        const int groups = (n0 % 128 + p.bn + 127) / 128;
+        ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
+        for (int kb = k0; kb < k1; ++kb) {
+          ok = mbar_wait(&full[stage], phase, abort_flag);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t sf = smem_u32(smem + oSf + stage * kStageSf);
+          const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + stage * kSfCols);
+          // a stage's scale columns: W's two tiles of 4 blocks, then X's (8 columns each)
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            sf_copy(tsf + a * 4, sf_desc(sf + a * 512));
+            for (int g = 0; g < groups; ++g)
+              sf_copy(tsf + 8 + a * 8 + g * 4, sf_desc(sf + (1 + g) * kSfBytes + a * 512));
+          }
+          const uint64_t ad = umma_desc_sw128(smem_u32(smem + oA + stage * kABytes));
+          const uint64_t bd = umma_desc_sw128(smem_u32(smem + oB + stage * kBBytes));
+          // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
+          const uint32_t tx = tsf + 8 + static_cast<uint32_t>(n0 % 128) / 32;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)          // 64 k = 32 bytes along a row per step
+            umma_mxf4(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
+                      tx + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
+          umma_commit(&empty[stage]);
+          if (++stage == kStages) stage = 0, phase ^= 1;
+        }
+        if (!ok) break;
+        umma_commit(&tfull[buf]);
+        if (++buf == 2) buf = 0, acc_phase ^= 1;
+      }
+      if (!ok) {
+        report(p.status, FQ_ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const int r_in_tile = quarter * 32 + lane;
+    const int hw = (p.bn / 2 + 15) / 16 * 16;
+    const int h0 = half * hw, h1 = half ? p.bn : hw;
+    pdl_wait();
+    int buf = 0;
+    uint32_t acc_phase = 0;
+    for (int u = first; u < p.units; u += step) {
+      const int row = u / p.TT * kBM + r_in_tile, n0 = u % p.TT * p.bn;
+      if (k0 < k1) {
+        // the warp leaves as one: the TMEM loads are warp-wide
+        if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
+          report(p.status, FQ_ERR_TIMEOUT);
+          *abort_flag = 1;
+          break;
+        }
+        tc_fence_after_sync();
+      }
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) +
+                             static_cast<uint32_t>(buf * kBN);
+      const int cols = min(h1, p.M - n0);
+#pragma unroll 1
+      for (int c = h0; c < cols; c += 16) {
+        float v[16];
+        __syncwarp();
+        if (k0 < k1) {
+          tmem_ld16(t_row + c, v);
+          tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[q] = 0.f;
+        }
+        if (SPLIT) {
+          // this rank's part, token major, over the stages: all of their copies and MMAs are done
+          float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+          for (int q = 0; q < 16; ++q) part[(c + q) * kBM + r_in_tile] = v[q];
+        } else if (row < p.R) {
+          __nv_bfloat16* dst = p.y + static_cast<int64_t>(n0 + c) * p.R + row;
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            if (c + q < cols) dst[static_cast<int64_t>(q) * p.R] = __float2bfloat16_rn(v[q]);
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty[buf]);
+      if (++buf == 2) buf = 0, acc_phase ^= 1;
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (SPLIT) {
+    cluster_sync();
+    // token c of the tile is finished by rank c mod KS: parts added in rank order
+    const int n0 = first % p.TT * p.bn, rt = first / p.TT;
+    const int tokens = min(p.bn, p.M - n0);
+    const uint32_t mine = smem_u32(smem);
+    if (!*abort_flag) {
+      for (int i = threadIdx.x; i < kBM * ((tokens - rank + p.KS - 1) / p.KS); i += kThreads) {
+        const int r = i % kBM, c = i / kBM * p.KS + rank;
+        const uint32_t at = mine + static_cast<uint32_t>(c * kBM + r) * 4;
+        float s = 0.f;
+        for (int q = 0; q < p.KS; ++q) s += ld_cluster_f32(mapa(at, static_cast<uint32_t>(q)));
+        if (rt * kBM + r < p.R)
+          p.y[static_cast<int64_t>(n0 + c) * p.R + rt * kBM + r] = __float2bfloat16_rn(s);
+      }
+    }
+    cluster_sync();
+  }
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// quantisation
+// ---------------------------------------------------------------------------------------------
+// Two values to E2M1 codes: to nearest, ties to the even code, saturating; hi in bits 4-7.
+__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 t;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
+      "cvt.u32.u8 %0, t;\n\t}"
+      : "=r"(r)
+      : "f"(lo), "f"(hi));
+  return r;
+}
+
+// Bytes of a tiled row group of scales: KB stages of 1 KiB.
+__device__ __forceinline__ int64_t scale_at(int row, int block, int KB) {
+  return (static_cast<int64_t>(row >> 7) * KB + (block >> 3)) * kSfBytes + (block >> 2 & 1) * 512 +
+         (row & 31) * 16 + (row >> 5 & 3) * 4 + (block & 3);
+}
+
+// Four threads to a block of 32 values, 16 to a word of four scales.  The grid covers the padded
+// rows and blocks too, whose scales are 0.
+constexpr int kQThreads = 256;
+
+__global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x, int rows,
+                                                                  int cols, int KB,
+                                                                  uint32_t* codes,
+                                                                  uint8_t* scales) {
+  // A kernel that follows may start once everything before this one is complete.
+  pdl_wait();
+  pdl_launch_dependents();
+  const int per_row = KB * 32;                    // threads along a padded row (8 values each)
+  const int64_t n = static_cast<int64_t>((rows + 127) / 128 * 128) * per_row;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(kQThreads) + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * kQThreads) {
+    const int row = static_cast<int>(i / per_row), t = static_cast<int>(i % per_row);
+    const bool in = row < rows && t * 8 < cols;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (in) v = __ldcg(x + static_cast<int64_t>(row) * (cols / 8) + t);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t m2 = 0;                              // largest magnitudes of even and odd values
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m2 = __vmaxu2(m2, w[q] & 0x7fff7fffu);
+    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
+    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
+    const uint32_t ex = max(m2 & 0xffffu, m2 >> 16) >> 7;
+    const bool fine = ex != 255;                  // no infinity and no NaN
+    const uint32_t sc = fine ? (ex > 2 ? ex - 2 : 0) : 255u;
+    // 2^(127 - sc) without rounding: the multiplication is exact, or far below the first step
+    const float inv = __uint_as_float((254u - min(sc, 252u)) << 23);
+    uint32_t c = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float lo = __uint_as_float(w[q] << 16), hi = __uint_as_float(w[q] & 0xffff0000u);
+      c |= e2m1x2(lo * inv, hi * inv) << (8 * q);
+    }
+    if (in) codes[static_cast<int64_t>(row) * (cols / 8) + t] = fine ? c : 0u;
+    // four blocks' scales as one word
+    uint32_t word = sc << (8 * (t >> 2 & 3));
+    word |= __shfl_xor_sync(0xffffffffu, word, 4);
+    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+    if ((t & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_at(row, t >> 2, KB)) = word;
+  }
+}
+
+__global__ void __launch_bounds__(kQThreads) mxfp_dequantize_kernel(const uint32_t* codes,
+                                                                    const uint8_t* scales,
+                                                                    int rows, int cols, int KB,
+                                                                    uint4* y) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int per_row = cols / 8;
+  const int64_t n = static_cast<int64_t>(rows) * per_row;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(kQThreads) + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * kQThreads) {
+    const int row = static_cast<int>(i / per_row), t = static_cast<int>(i % per_row);
+    const uint32_t c = __ldcg(codes + i);
+    const uint32_t sc = __ldcg(scales + scale_at(row, t >> 2, KB));
+    const float scale = __uint_as_float(sc == 255 ? 0x7fc00000u : sc ? sc << 23 : 0x00400000u);
+    uint32_t o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t h2;                                // two E2M1 values as fp16, exact
+      asm("{\n\t.reg .b8 t;\n\t"
+          "cvt.u8.u32 t, %1;\n\t"
+          "cvt.rn.f16x2.e2m1x2 %0, t;\n\t}"
+          : "=r"(h2)
+          : "r"(c >> (8 * q) & 255u));
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
+      const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);
+      o[q] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    y[i] = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------
+PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000,
+                                         cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+  });
+  return fn;
+}
+
+// codes, rows x cols / 2 bytes, boxes of 128 bytes x box_rows under the 128-byte swizzle
+bool make_tmap(CUtensorMap* m, const void* base, int rows, int cols, int box_rows) {
+  auto enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols / 2), static_cast<cuuint64_t>(rows)};
+  cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols / 2)};
+  cuuint32_t box[2] = {kKStage / 2, static_cast<cuuint32_t>(box_rows)};
+  cuuint32_t estr[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box,
+             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+bool sizes_ok(int rows, int cols) { return rows > 0 && cols > 0 && cols % 32 == 0; }
+
+fq_status check_device(int& sms) {
+  int dev = 0, major = 0, minor = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+    return FQ_ERR_CUDA;
+  if (major * 10 + minor != 103) return FQ_ERR_UNSUPPORTED;
+  return cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+fq_status check_mxfp(const fq_mxfp* q) {
+  if (!q || !q->codes || !q->scales || !sizes_ok(q->rows, q->cols)) return FQ_ERR_INVALID_ARG;
+  return aligned16(q->codes) && aligned16(q->scales) ? FQ_OK : FQ_ERR_ALIGNMENT;
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, int cluster,
+                   cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(block));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+int stages_of(int cols) { return static_cast<int>(ceil_div(cols, kKStage)); }
+
+fq_status quantize(const void* x, const fq_mxfp& q, int sms, cudaStream_t s) {
+  const int KB = stages_of(q.cols);
+  const int64_t n = round_up(q.rows, 128) * KB * 32;
+  return launch(mxfp_quantize_kernel, std::min<int64_t>(ceil_div(n, kQThreads), 16ll * sms),
+                kQThreads, 0, 1, s, static_cast<const uint4*>(x), q.rows, q.cols, KB,
+                reinterpret_cast<uint32_t*>(q.codes), q.scales) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+template <bool SPLIT>
+fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProdArgs& a, int sms,
+                         cudaStream_t s) {
+  static std::mutex mu;
+  static std::map<int, bool> done;
+  {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
+    std::lock_guard<std::mutex> lock(mu);
+    if (!done[dev]) {
+      if (cudaFuncSetAttribute(mxfp_product_kernel<SPLIT>,
+                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               kSmemBytes) != cudaSuccess)
+        return FQ_ERR_CUDA;
+      done[dev] = true;
+    }
+  }
+  const int grid = SPLIT ? a.units * a.KS : std::min(a.units, sms);
+  return launch(mxfp_product_kernel<SPLIT>, grid, kThreads, kSmemBytes, SPLIT ? a.KS : 1, s, mw, mx,
+                a) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+// Tokens per tile: all of up to 192 in one tile.  More go by tiles of 128 or 192, whose first
+// token is a multiple of 64 (scales of X then start on an even column of their tile), whichever
+// wastes fewer columns, the wider of equals.
+int pick_bn(int M) {
+  if (M <= kBN) return static_cast<int>(round_up(M, 16));
+  return round_up(M, 128) < round_up(M, 192) ? 128 : 192;
+}
+
+fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, int sms,
+                  bool early_w, cudaStream_t s) {
+  ProdArgs a{};
+  a.R = W.rows;
+  a.M = X.rows;
+  a.bn = pick_bn(a.M);
+  a.RT = static_cast<int>(ceil_div(a.R, kBM));
+  a.TT = static_cast<int>(ceil_div(a.M, a.bn));
+  a.KB = stages_of(W.cols);
+  a.units = a.RT * a.TT;
+  a.KS = 1;
+  while (a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
+  a.kbs = static_cast<int>(ceil_div(a.KB, a.KS));
+  a.sw = W.scales;
+  a.sx = X.scales;
+  a.xgroups = static_cast<int>(ceil_div(a.M, 128));
+  a.early_w = early_w;
+  a.y = static_cast<__nv_bfloat16*>(y);
+  a.status = status;
+  CUtensorMap mw, mx;
+  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM) || !make_tmap(&mx, X.codes, X.rows, X.cols, a.bn))
+    return FQ_ERR_CUDA;
+  return a.KS > 1 ? launch_product<true>(mw, mx, a, sms, s)
+                  : launch_product<false>(mw, mx, a, sms, s);
+}
+
+struct Ws {
+  size_t codes, scales, total;
+};
+
+Ws ws_layout(int M, int d_in) {
+  Ws L{};
+  L.codes = 256;
+  L.scales = L.codes + round_up(static_cast<int64_t>(fq_mxfp_codes_bytes(M, d_in)), 256);
+  L.total = L.scales + round_up(static_cast<int64_t>(fq_mxfp_scales_bytes(M, d_in)), 256);
+  return L;
+}
+
+}  // namespace
+}  // namespace fq
+
+using namespace fq;
+
+extern "C" {
+
+size_t fq_mxfp_codes_bytes(int rows, int cols) {
+  return sizes_ok(rows, cols) ? static_cast<size_t>(rows) * (cols / 2) : 0;
+}
+
+size_t fq_mxfp_scales_bytes(int rows, int cols) {
+  if (!sizes_ok(rows, cols)) return 0;
+  return static_cast<size_t>(ceil_div(rows, 128)) * stages_of(cols) * kSfBytes;
+}
+
+fq_status fq_mxfp_quantize(const void* x, int rows, int cols, const fq_mxfp* q,
+                           fq_stream_t stream) {
+  if (!x || !sizes_ok(rows, cols)) return FQ_ERR_INVALID_ARG;
+  if (const fq_status st = check_mxfp(q)) return st;
+  if (q->rows != rows || q->cols != cols) return FQ_ERR_INVALID_ARG;
+  if (!aligned16(x)) return FQ_ERR_ALIGNMENT;
+  int sms = 0;
+  if (const fq_status st = check_device(sms)) return st;
+  return quantize(x, *q, sms, reinterpret_cast<cudaStream_t>(stream));
+}
+
+fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream) {
+  if (!y) return FQ_ERR_INVALID_ARG;
+  if (const fq_status st = check_mxfp(q)) return st;
+  if (!aligned16(y)) return FQ_ERR_ALIGNMENT;
+  int sms = 0;
+  if (const fq_status st = check_device(sms)) return st;
+  const int64_t n = static_cast<int64_t>(q->rows) * (q->cols / 8);
+  return launch(mxfp_dequantize_kernel, std::min<int64_t>(ceil_div(n, kQThreads), 16ll * sms),
+                kQThreads, 0, 1, reinterpret_cast<cudaStream_t>(stream),
+                reinterpret_cast<const uint32_t*>(q->codes),
+                static_cast<const uint8_t*>(q->scales), q->rows, q->cols, stages_of(q->cols),
+                static_cast<uint4*>(y)) == cudaSuccess
+             ? FQ_OK
+             : FQ_ERR_CUDA;
+}
+
+fq_status fq_mxfp_product(const fq_mxfp* X, const fq_mxfp* W, void* y, int32_t* status,
+                          fq_stream_t stream) {
+  if (!y) return FQ_ERR_INVALID_ARG;
+  if (const fq_status st = check_mxfp(X)) return st;
+  if (const fq_status st = check_mxfp(W)) return st;
+  if (X->cols != W->cols) return FQ_ERR_INVALID_ARG;
+  if (!aligned16(y) || (status && reinterpret_cast<uintptr_t>(status) % 4)) return FQ_ERR_ALIGNMENT;
+  int sms = 0;
+  if (const fq_status st = check_device(sms)) return st;
+  return product(*X, *W, y, status, sms, false, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t fq_mxfp_workspace_bytes(int M, int d_in, int d_out) {
+  if (!sizes_ok(M, d_in) || d_out <= 0) return 0;
+  return ws_layout(M, d_in).total;
+}
+
+fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void* y, void* ws,
+                         size_t ws_bytes, fq_stream_t stream) {
+  if (!x || !y || !sizes_ok(M, d_in)) return FQ_ERR_INVALID_ARG;
+  if (const fq_status st = check_mxfp(W)) return st;
+  if (W->cols != d_in) return FQ_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(y)) return FQ_ERR_ALIGNMENT;
+  if (!ws) return FQ_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return FQ_ERR_ALIGNMENT;
+  if (ws_bytes < fq_mxfp_workspace_bytes(M, d_in, W->rows)) return FQ_ERR_WORKSPACE;
+  int sms = 0;
+  if (const fq_status st = check_device(sms)) return st;
+  const Ws L = ws_layout(M, d_in);
+  auto* w = static_cast<uint8_t*>(ws);
+  const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
+  auto s = reinterpret_cast<cudaStream_t>(stream);
+  if (const fq_status st = quantize(x, X, sms, s)) return st;
+  return product(X, *W, y, static_cast<int32_t*>(ws), sms, true, s);
+}
+
+}  // extern "C"
