@@ -2,19 +2,27 @@
 // two quantised matrices on the block-scaled tensor cores (kind::mxf4: E2M1 operands, one
 // power-of-two scale per row and 32 k, fp32 accumulation).
 //
-// Product: y[t][i] = sum_k W[i][k] X[t][k].  A tile is 128 rows of W (the accumulator's rows) x
-// bn <= 192 tokens.  Codes arrive by TMA, 256 k (128 bytes) a stage under the 128-byte swizzle;
-// scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage, and go
-// through shared memory into TMEM (tcgen05.cp) ahead of the stage's four MMAs of 64 k.  Of the
-// 512 TMEM columns two accumulators take 2 x 192 and every stage has 24 of its own for scales,
-// so no copy waits for an MMA other than its stage's last user.
+// Product: y[t][i] = sum_k W[i][k] X[t][k].  A tile is CG * 128 rows of W (the accumulator's
+// rows) x bn <= 192 tokens.  Codes arrive by TMA, 256 k (128 bytes) a stage under the 128-byte
+// swizzle; scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage.  Of
+// the 512 TMEM columns two accumulators take 2 x 192 and every stage has 24 of its own for its
+// scales.
+//
+// Scales go from shared memory into TMEM by four warps with tcgen05.st.  tcgen05.cp, issued
+// between the MMAs, takes its turn in their pipe: six copies a stage made 725 cycles of the 384
+// that the stage's four MMAs of 128 x 192 x 64 take, the stores none.
+//
+// With CG = 2 a cluster of two CTAs works on 256 x bn: each stages its 128 rows of W and half of
+// the tokens' codes, one MMA reads both CTAs' shared memory.  At four times the bf16 rate the
+// tiles' traffic from L2 is what bounds a large product, and this cuts it by 28%.
 //
 // Few tokens read W once at memory speed; the tiles are then too few for the SMs, so a cluster of
 // KS CTAs splits the k range of one tile and adds the parts up, in rank order, through
 // distributed shared memory.
 //
-// Warp roles: warp 0 producer (one lane), warp 1 TMEM owner + MMA issuer (one lane), warps 2-9
-// epilogue (thread = accumulator row, half of the tokens).
+// Warp roles: warp 0 producer (one lane), warp 1 TMEM owner + MMA issuer (one lane, of the first
+// CTA of a pair), warps 2-9 epilogue (thread = accumulator row, half of the tokens), warps 10-13
+// scales.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -33,21 +41,22 @@ constexpr int kBM = 128;                        // rows of W per tile
 constexpr int kBN = 192;                        // tokens per tile, at most
 constexpr int kKStage = 256;                    // k per stage: 128 bytes of codes a row
 constexpr int kABytes = kBM * kKStage / 2;
-constexpr int kBBytes = kBN * kKStage / 2;
 constexpr int kSfBytes = 1024;                  // scales of 128 rows x 256 k
 constexpr int kStageSf = 3 * kSfBytes;          // W's, and up to two row groups of X's
 constexpr int kStages = 5;
-constexpr int kThreads = 320;
+constexpr int kThreads = 448;
 constexpr int kTmemCols = 512;
 constexpr int kSfCol = 2 * kBN;                 // TMEM columns of the scales, 24 a stage
 constexpr int kSfCols = 24;
 static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "tensor memory");
 
+constexpr int kBBytes = kBN * kKStage / 2;      // CG = 1; a CTA of a pair uses half of it
+
 constexpr int oA = 0;
 constexpr int oB = oA + kStages * kABytes;
 constexpr int oSf = oB + kStages * kBBytes;
 constexpr int oBar = oSf + kStages * kStageSf;
-constexpr int oMisc = oBar + (2 * kStages + 4) * 8;
+constexpr int oMisc = oBar + (4 * kStages + 4) * 8;
 constexpr int kSmemBytes = oMisc + 16 + 1024;   // + alignment slack
 static_assert(kSmemBytes <= 227 * 1024, "shared memory");
 static_assert(kBN * kBM * 4 <= oBar, "a tile's fp32 part fits the stages");
@@ -59,46 +68,49 @@ struct ProdArgs {
   int units;                  // tiles (KS == 1)
   const uint8_t* sw;          // scales of W, of X: 1 KiB per row group and stage
   const uint8_t* sx;
-  int xgroups;                // row groups of X's scales
+  int wgroups, xgroups;       // row groups of W's and of X's scales
   int early_w;                // W does not depend on the kernel before this one
   __nv_bfloat16* y;
   int32_t* status;
 };
 
-// Shared-memory descriptor of 32 x 128-bit scale rows without swizzle: 8 rows of 16 bytes are
-// 128 contiguous bytes, and so are the next 8 (stride byte offset 128).
-__device__ __forceinline__ uint64_t sf_desc(uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((smem_addr >> 4) & 0x3FFF);
-  d |= static_cast<uint64_t>(1) << 16;
-  d |= static_cast<uint64_t>(128 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  return d;
-}
-
-// 512 bytes of scales (128 rows x 4) -> 4 TMEM columns, in all four lane quarters.
-__device__ __forceinline__ void sf_copy(uint32_t tmem, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc)
+// 512 bytes of scales (128 rows x 4, 16 bytes to the four rows l, l + 32, ...) -> 4 TMEM columns
+// of this warp's lane quarter.
+__device__ __forceinline__ void sf_store(uint32_t tmem, const uint8_t* src, int lane) {
+  const uint4 v = *reinterpret_cast<const uint4*>(src + lane * 16);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem),
+               "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
 }
 
 // Instruction descriptor, kind::mxf4: E2M1 A and B (1), power-of-two scales (bit 23), fp32
-// accumulator, both K-major, 128 x N; sf: which pair of the scale words' four bytes (0 or 2).
-__device__ __forceinline__ uint32_t idesc_mxf4(uint32_t N, uint32_t sf) {
-  return (sf << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) |
-         ((static_cast<uint32_t>(kBM) >> 4) << 24) | (sf << 29);
+// accumulator, both K-major, M x N; sf: which pair of the scale words' four bytes (0 or 2).
+__device__ __forceinline__ uint32_t idesc_mxf4(uint32_t M, uint32_t N, uint32_t sf) {
+  return (sf << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (1u << 23) | ((M >> 4) << 24) |
+         (sf << 29);
 }
 
+template <int CG>
 __device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc,
                                           uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
-      "[%5], p;\n\t}" ::"r"(tmem_d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
-      : "memory");
+  if constexpr (CG == 1) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
+        "[%5], p;\n\t}" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], "
+        "[%5], p;\n\t}" ::"r"(tmem_d),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+  }
 }
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
@@ -107,81 +119,109 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return v;
 }
 
-template <bool SPLIT>
+template <int CG, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
     mxfp_product_kernel(const __grid_constant__ CUtensorMap tmW,
                         const __grid_constant__ CUtensorMap tmX, const ProdArgs p) {
+  static_assert(CG == 1 || !SPLIT, "a pair does not split its tile's k");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);   // codes of both CTAs (first CTA's)
   uint64_t* empty = full + kStages;
-  uint64_t* tfull = empty + kStages;
-  uint64_t* tempty = tfull + 2;
+  uint64_t* sfull = empty + kStages;                           // this CTA's scales in smem
+  uint64_t* sready = sfull + kStages;                          // scales in TMEM (first CTA's)
+  uint64_t* tfull = sready + kStages;
+  uint64_t* tempty = tfull + 2;                                // used in the pair's first CTA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + oMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // SPLIT: one tile per cluster, its k range over the ranks; else tiles in turn
-  const int rank = SPLIT ? static_cast<int>(cluster_ctarank()) : 0;
-  const int first = SPLIT ? static_cast<int>(blockIdx.x) / p.KS : static_cast<int>(blockIdx.x);
-  const int step = SPLIT ? p.units : static_cast<int>(gridDim.x);
+  const int rank = SPLIT || CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int first = static_cast<int>(blockIdx.x) / (SPLIT ? p.KS : CG);
+  const int step = SPLIT ? p.units : static_cast<int>(gridDim.x) / CG;
   const int k0 = SPLIT ? min(p.KB, rank * p.kbs) : 0;
   const int k1 = SPLIT ? min(p.KB, k0 + p.kbs) : p.KB;
   // tile u = row tile * TT + token tile: the CTAs of a wave share W's tiles
+  auto tile_n0 = [&](int u) { return u % p.TT * p.bn; };
+  // first row group (128 rows) of this CTA's part of W
+  auto tile_rg = [&](int u) { return u / p.TT * CG + (CG == 2 ? rank : 0); };
+  // row groups of X's scales that a tile touches and that exist
+  auto groups_of = [&](int n0) { return min(p.xgroups, (n0 + p.bn + 127) / 128) - n0 / 128; };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
+      mbar_init(&sfull[s], 1);
+      mbar_init(&sready[s], 4 * CG);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
-      mbar_init(&tempty[b], 8);
+      mbar_init(&tempty[b], 8 * CG);
     }
     *abort_flag = 0;
     fence_barrier_init();
     prefetch_tmap(&tmW);
     prefetch_tmap(&tmX);
   }
-  if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+  if (warp == 1) tmem_alloc_cg<CG>(tmem_slot, kTmemCols);
   tc_fence_before_sync();
   __syncthreads();
+  if (CG == 2) cluster_sync();
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
+
+  // arrive on a barrier of the pair's first CTA (one lane)
+  auto arrive_first = [&](uint64_t* bar) {
+    if (CG == 2) mbar_arrive_cluster(mapa(smem_u32(bar), 0));
+    else mbar_arrive(bar);
+  };
+  auto timed_out = [&]() {
+    report(p.status, FQ_ERR_TIMEOUT);
+    *abort_flag = 1;
+  };
 
   if (warp == 0) {
     // ---------------------------------------------------------------- producer
     if (lane == 0) {
       const uint64_t pol_x = policy_evict_last();
       const uint64_t pol_w = p.TT == 1 ? policy_evict_first() : pol_x;
-      auto load_w = [&](int st, int rt, int kb) {
-        tma_load_2d(smem + oA + st * kABytes, &tmW, &full[st], kb * (kKStage / 2), rt * kBM,
-                    pol_w);
-        bulk_load(smem + oSf + st * kStageSf, p.sw + (static_cast<int64_t>(rt) * p.KB + kb) * kSfBytes,
-                  kSfBytes, &full[st], pol_w);
+      const int bn_cta = p.bn / CG;
+      const uint32_t bytes = static_cast<uint32_t>(kABytes + bn_cta * (kKStage / 2));
+      auto load = [&](uint8_t* dst, const CUtensorMap* tm, int st, int x, int y, uint64_t pol) {
+        if (CG == 2) tma_load_2d_pair(dst, tm, mapa(smem_u32(&full[st]), 0), x, y, pol);
+        else tma_load_2d(dst, tm, &full[st], x, y, pol);
+      };
+      auto expect = [&](int st, int groups) {
+        // the first CTA expects the codes of both (the other's may arrive before)
+        if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&full[st], CG * bytes);
+        mbar_arrive_expect_tx(&sfull[st], static_cast<uint32_t>((1 + groups) * kSfBytes));
+      };
+      auto load_w = [&](int st, int u, int kb) {
+        const int rg = tile_rg(u);
+        load(smem + oA + st * kABytes, &tmW, st, kb * (kKStage / 2), rg * kBM, pol_w);
+        // a pair's second half may lie beyond the last row group: its rows are not used
+        bulk_load(smem + oSf + st * kStageSf,
+                  p.sw + (static_cast<int64_t>(min(rg, p.wgroups - 1)) * p.KB + kb) * kSfBytes,
+                  kSfBytes, &sfull[st], pol_w);
       };
       auto load_x = [&](int st, int n0, int groups, int kb) {
-        tma_load_2d(smem + oB + st * kBBytes, &tmX, &full[st], kb * (kKStage / 2), n0, pol_x);
+        load(smem + oB + st * kBBytes, &tmX, st, kb * (kKStage / 2),
+             n0 + (CG == 2 ? rank * bn_cta : 0), pol_x);
         for (int g = 0; g < groups; ++g)
           bulk_load(smem + oSf + st * kStageSf + (1 + g) * kSfBytes,
                     p.sx + (static_cast<int64_t>(n0 / 128 + g) * p.KB + kb) * kSfBytes, kSfBytes,
-                    &full[st], pol_x);
-      };
-      // row groups of X's scales that a tile touches and that exist
-      auto groups_of = [&](int n0) {
-        return min(p.xgroups, (n0 + p.bn + 127) / 128) - n0 / 128;
-      };
-      auto bytes_of = [&](int groups) {
-        return static_cast<uint32_t>(kABytes + p.bn * (kKStage / 2) + (1 + groups) * kSfBytes);
+                    &sfull[st], pol_x);
       };
       int pre = 0;
       if (p.early_w && first < p.units) {
         pre = min(kStages, k1 - k0);
         for (int i = 0; i < pre; ++i) {
-          mbar_arrive_expect_tx(&full[i], bytes_of(groups_of(first % p.TT * p.bn)));
-          load_w(i, first / p.TT, k0 + i);
+          expect(i, groups_of(tile_n0(first)));
+          load_w(i, first, k0 + i);
         }
       }
       pdl_wait();
@@ -190,16 +230,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t phase = 0;
       int64_t it = 0;
       for (int u = first; u < p.units && !*abort_flag; u += step) {
-        const int rt = u / p.TT, n0 = u % p.TT * p.bn, groups = groups_of(n0);
+        const int n0 = tile_n0(u), groups = groups_of(n0);
         for (int kb = k0; kb < k1; ++kb, ++it) {
           if (it >= pre) {
             if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
-              report(p.status, FQ_ERR_TIMEOUT);
-              *abort_flag = 1;
+              timed_out();
               break;
             }
-            mbar_arrive_expect_tx(&full[stage], bytes_of(groups));
-            load_w(stage, rt, kb);
+            expect(stage, groups);
+            load_w(stage, u, kb);
           }
           load_x(stage, n0, groups, kb);
           if (++stage == kStages) stage = 0, phase ^= 1;
@@ -214,52 +253,71 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
-      const uint32_t id0 = idesc_mxf4(static_cast<uint32_t>(p.bn), 0);
-      const uint32_t id2 = idesc_mxf4(static_cast<uint32_t>(p.bn), 2);
+    if (lane == 0 && (CG == 1 || rank == 0)) {
+      const uint32_t id0 = idesc_mxf4(CG * kBM, static_cast<uint32_t>(p.bn), 0);
+      const uint32_t id2 = idesc_mxf4(CG * kBM, static_cast<uint32_t>(p.bn), 2);
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
       for (int u = first; ok && k0 < k1 && u < p.units && !*abort_flag; u += step) {
-        const int n0 = u % p.TT * p.bn;
-        const int groups = (n0 % 128 + p.bn + 127) / 128;
         ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
+        // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
+        const uint32_t shift = 8 + static_cast<uint32_t>(tile_n0(u) % 128) / 32;
         for (int kb = k0; kb < k1; ++kb) {
-          ok = mbar_wait(&full[stage], phase, abort_flag);
+          ok = mbar_wait(&full[stage], phase, abort_flag) &&
+               mbar_wait(&sready[stage], phase, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t sf = smem_u32(smem + oSf + stage * kStageSf);
           const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + stage * kSfCols);
-          // a stage's scale columns: W's two tiles of 4 blocks, then X's (8 columns each)
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            sf_copy(tsf + a * 4, sf_desc(sf + a * 512));
-            for (int g = 0; g < groups; ++g)
-              sf_copy(tsf + 8 + a * 8 + g * 4, sf_desc(sf + (1 + g) * kSfBytes + a * 512));
-          }
           const uint64_t ad = umma_desc_sw128(smem_u32(smem + oA + stage * kABytes));
           const uint64_t bd = umma_desc_sw128(smem_u32(smem + oB + stage * kBBytes));
-          // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
-          const uint32_t tx = tsf + 8 + static_cast<uint32_t>(n0 % 128) / 32;
 #pragma unroll
           for (int j = 0; j < 4; ++j)          // 64 k = 32 bytes along a row per step
-            umma_mxf4(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
-                      tx + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
-          umma_commit(&empty[stage]);
+            umma_mxf4<CG>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
+                          tsf + shift + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
+          umma_commit_cg<CG>(&empty[stage]);
           if (++stage == kStages) stage = 0, phase ^= 1;
         }
         if (!ok) break;
-        umma_commit(&tfull[buf]);
+        umma_commit_cg<CG>(&tfull[buf]);
         if (++buf == 2) buf = 0, acc_phase ^= 1;
       }
-      if (!ok) {
-        report(p.status, FQ_ERR_TIMEOUT);
-        *abort_flag = 1;
+      if (!ok) timed_out();
+    }
+  } else if (warp >= 10) {
+    // ---------------------------------------------------------------- scales
+    // A stage's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).  Its last MMAs
+    // are done once its next copies have been issued, so sfull covers them too.
+    const uint32_t t_sf = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kSfCol;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int u = first; ok && u < p.units; u += step) {
+      const int groups = groups_of(tile_n0(u));
+      for (int kb = k0; kb < k1; ++kb) {
+        // the warp leaves as one: the TMEM stores are warp-wide
+        ok = __all_sync(0xffffffffu, mbar_wait(&sfull[stage], phase, abort_flag));
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint8_t* sf = smem + oSf + stage * kStageSf;
+        const uint32_t t = t_sf + static_cast<uint32_t>(stage * kSfCols);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          sf_store(t + a * 4, sf + a * 512, lane);
+          for (int g = 0; g < groups; ++g)
+            sf_store(t + 8 + a * 8 + g * 4, sf + (1 + g) * kSfBytes + a * 512, lane);
+        }
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) arrive_first(&sready[stage]);
+        if (++stage == kStages) stage = 0, phase ^= 1;
       }
     }
+    if (!ok) timed_out();
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -270,12 +328,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     int buf = 0;
     uint32_t acc_phase = 0;
     for (int u = first; u < p.units; u += step) {
-      const int row = u / p.TT * kBM + r_in_tile, n0 = u % p.TT * p.bn;
+      const int row = tile_rg(u) * kBM + r_in_tile, n0 = tile_n0(u);
       if (k0 < k1) {
         // the warp leaves as one: the TMEM loads are warp-wide
         if (!__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
-          report(p.status, FQ_ERR_TIMEOUT);
-          *abort_flag = 1;
+          timed_out();
           break;
         }
         tc_fence_after_sync();
@@ -308,17 +365,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty[buf]);
+      if (lane == 0) arrive_first(&tempty[buf]);
       if (++buf == 2) buf = 0, acc_phase ^= 1;
     }
   }
 
   tc_fence_before_sync();
   __syncthreads();
+  if (CG == 2) cluster_sync();
   if (SPLIT) {
     cluster_sync();
     // token c of the tile is finished by rank c mod KS: parts added in rank order
-    const int n0 = first % p.TT * p.bn, rt = first / p.TT;
+    const int n0 = tile_n0(first), row0 = tile_rg(first) * kBM;
     const int tokens = min(p.bn, p.M - n0);
     const uint32_t mine = smem_u32(smem);
     if (!*abort_flag) {
@@ -327,15 +385,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t at = mine + static_cast<uint32_t>(c * kBM + r) * 4;
         float s = 0.f;
         for (int q = 0; q < p.KS; ++q) s += ld_cluster_f32(mapa(at, static_cast<uint32_t>(q)));
-        if (rt * kBM + r < p.R)
-          p.y[static_cast<int64_t>(n0 + c) * p.R + rt * kBM + r] = __float2bfloat16_rn(s);
+        if (row0 + r < p.R)
+          p.y[static_cast<int64_t>(n0 + c) * p.R + row0 + r] = __float2bfloat16_rn(s);
       }
     }
     cluster_sync();
   }
   if (warp == 1) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem_base, kTmemCols);
+    tmem_dealloc_cg<CG>(tmem_base, kTmemCols);
   }
 }
 
@@ -353,16 +411,26 @@ __device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
   return r;
 }
 
-// Bytes of a tiled row group of scales: KB stages of 1 KiB.
-__device__ __forceinline__ int64_t scale_at(int row, int block, int KB) {
-  return (static_cast<int64_t>(row >> 7) * KB + (block >> 3)) * kSfBytes + (block >> 2 & 1) * 512 +
-         (row & 31) * 16 + (row >> 5 & 3) * 4 + (block & 3);
-}
-
-// Four threads to a block of 32 values, 16 to a word of four scales.  The grid covers the padded
-// rows and blocks too, whose scales are 0.
+// A block of threads covers 8 x 4 rows by one stage of 256 columns: a warp is a row of 256 values
+// (8 a thread), and a thread has the rows r, r + 32, r + 64, r + 96 of a group of 128, so that its
+// four loads are in flight together and their scales, which lie side by side, move as 16 bytes.
+// Four threads make a block of 32 values, 16 a tile of 4 blocks.
 constexpr int kQThreads = 256;
 
+struct QPlace {
+  int row, block;                                 // first of the four rows; thread along the row
+  int64_t scales;                                 // the 16 bytes of its tile
+};
+
+__device__ __forceinline__ QPlace q_place(int KB) {
+  const int lane = threadIdx.x & 31;
+  const int group = blockIdx.x >> 2, r = (blockIdx.x & 3) * 8 + (threadIdx.x >> 5);
+  const int kb = blockIdx.y;
+  return {group * 128 + r, kb * 32 + lane,
+          (static_cast<int64_t>(group) * KB + kb) * kSfBytes + (lane >> 4) * 512 + r * 16};
+}
+
+// The grid covers the padded rows and blocks too, whose scales are 0.
 __global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x, int rows,
                                                                   int cols, int KB,
                                                                   uint32_t* codes,
@@ -370,15 +438,19 @@ __global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x
   // A kernel that follows may start once everything before this one is complete.
   pdl_wait();
   pdl_launch_dependents();
-  const int per_row = KB * 32;                    // threads along a padded row (8 values each)
-  const int64_t n = static_cast<int64_t>((rows + 127) / 128 * 128) * per_row;
-  for (int64_t i = blockIdx.x * static_cast<int64_t>(kQThreads) + threadIdx.x; i < n;
-       i += static_cast<int64_t>(gridDim.x) * kQThreads) {
-    const int row = static_cast<int>(i / per_row), t = static_cast<int>(i % per_row);
-    const bool in = row < rows && t * 8 < cols;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (in) v = __ldcg(x + static_cast<int64_t>(row) * (cols / 8) + t);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  const QPlace at = q_place(KB);
+  const bool in_col = at.block * 8 < cols;
+  uint4 v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = at.row + 32 * j;
+    v[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (in_col && row < rows) v[j] = __ldcg(x + static_cast<int64_t>(row) * (cols / 8) + at.block);
+  }
+  uint32_t words[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
     uint32_t m2 = 0;                              // largest magnitudes of even and odd values
 #pragma unroll
     for (int q = 0; q < 4; ++q) m2 = __vmaxu2(m2, w[q] & 0x7fff7fffu);
@@ -387,7 +459,7 @@ __global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x
     const uint32_t ex = max(m2 & 0xffffu, m2 >> 16) >> 7;
     const bool fine = ex != 255;                  // no infinity and no NaN
     const uint32_t sc = fine ? (ex > 2 ? ex - 2 : 0) : 255u;
-    // 2^(127 - sc) without rounding: the multiplication is exact, or far below the first step
+    // 2^(127 - sc): the multiplication is exact, or far below the first step
     const float inv = __uint_as_float((254u - min(sc, 252u)) << 23);
     uint32_t c = 0;
 #pragma unroll
@@ -395,13 +467,18 @@ __global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x
       const float lo = __uint_as_float(w[q] << 16), hi = __uint_as_float(w[q] & 0xffff0000u);
       c |= e2m1x2(lo * inv, hi * inv) << (8 * q);
     }
-    if (in) codes[static_cast<int64_t>(row) * (cols / 8) + t] = fine ? c : 0u;
+    const int row = at.row + 32 * j;
+    if (in_col && row < rows)
+      codes[static_cast<int64_t>(row) * (cols / 8) + at.block] = fine ? c : 0u;
     // four blocks' scales as one word
-    uint32_t word = sc << (8 * (t >> 2 & 3));
+    uint32_t word = sc << (8 * (threadIdx.x >> 2 & 3));
     word |= __shfl_xor_sync(0xffffffffu, word, 4);
     word |= __shfl_xor_sync(0xffffffffu, word, 8);
-    if ((t & 15) == 0) *reinterpret_cast<uint32_t*>(scales + scale_at(row, t >> 2, KB)) = word;
+    words[j] = word;
   }
+  if ((threadIdx.x & 15) == 0)
+    *reinterpret_cast<uint4*>(scales + at.scales) =
+        make_uint4(words[0], words[1], words[2], words[3]);
 }
 
 __global__ void __launch_bounds__(kQThreads) mxfp_dequantize_kernel(const uint32_t* codes,
@@ -410,13 +487,21 @@ __global__ void __launch_bounds__(kQThreads) mxfp_dequantize_kernel(const uint32
                                                                     uint4* y) {
   pdl_launch_dependents();
   pdl_wait();
-  const int per_row = cols / 8;
-  const int64_t n = static_cast<int64_t>(rows) * per_row;
-  for (int64_t i = blockIdx.x * static_cast<int64_t>(kQThreads) + threadIdx.x; i < n;
-       i += static_cast<int64_t>(gridDim.x) * kQThreads) {
-    const int row = static_cast<int>(i / per_row), t = static_cast<int>(i % per_row);
-    const uint32_t c = __ldcg(codes + i);
-    const uint32_t sc = __ldcg(scales + scale_at(row, t >> 2, KB));
+  const QPlace at = q_place(KB);
+  if (at.block * 8 >= cols) return;
+  const uint4 s4 = __ldcg(reinterpret_cast<const uint4*>(scales + at.scales));
+  const uint32_t words[4] = {s4.x, s4.y, s4.z, s4.w};
+  uint32_t code[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = at.row + 32 * j;
+    if (row < rows) code[j] = __ldcg(codes + static_cast<int64_t>(row) * (cols / 8) + at.block);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int row = at.row + 32 * j;
+    if (row >= rows) break;
+    const uint32_t sc = words[j] >> (8 * (threadIdx.x >> 2 & 3)) & 255u;
     const float scale = __uint_as_float(sc == 255 ? 0x7fc00000u : sc ? sc << 23 : 0x00400000u);
     uint32_t o[4];
 #pragma unroll
@@ -426,12 +511,12 @@ __global__ void __launch_bounds__(kQThreads) mxfp_dequantize_kernel(const uint32
           "cvt.u8.u32 t, %1;\n\t"
           "cvt.rn.f16x2.e2m1x2 %0, t;\n\t}"
           : "=r"(h2)
-          : "r"(c >> (8 * q) & 255u));
+          : "r"(code[j] >> (8 * q) & 255u));
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h2));
       const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);
       o[q] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    y[i] = make_uint4(o[0], o[1], o[2], o[3]);
+    y[static_cast<int64_t>(row) * (cols / 8) + at.block] = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
@@ -488,10 +573,10 @@ fq_status check_mxfp(const fq_mxfp* q) {
 }
 
 template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, int cluster,
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, int block, size_t smem, int cluster,
                    cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(block));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -509,36 +594,66 @@ cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t sm
 
 int stages_of(int cols) { return static_cast<int>(ceil_div(cols, kKStage)); }
 
-fq_status quantize(const void* x, const fq_mxfp& q, int sms, cudaStream_t s) {
+dim3 q_grid(int rows, int KB) {
+  return dim3(static_cast<unsigned>(ceil_div(rows, 128) * 4), static_cast<unsigned>(KB));
+}
+
+fq_status quantize(const void* x, const fq_mxfp& q, cudaStream_t s) {
   const int KB = stages_of(q.cols);
-  const int64_t n = round_up(q.rows, 128) * KB * 32;
-  return launch(mxfp_quantize_kernel, std::min<int64_t>(ceil_div(n, kQThreads), 16ll * sms),
-                kQThreads, 0, 1, s, static_cast<const uint4*>(x), q.rows, q.cols, KB,
+  return launch(mxfp_quantize_kernel, q_grid(q.rows, KB), kQThreads, 0, 1, s, static_cast<const uint4*>(x), q.rows, q.cols, KB,
                 reinterpret_cast<uint32_t*>(q.codes), q.scales) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
 
-template <bool SPLIT>
+// CTAs (CG = 2: pairs) that the device runs at once.
+template <int CG, bool SPLIT>
+fq_status prepare_product(int sms, int& room) {
+  static std::mutex mu;
+  static std::map<int, int> fit;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
+  std::lock_guard<std::mutex> lock(mu);
+  auto it = fit.find(dev);
+  if (it == fit.end()) {
+    if (cudaFuncSetAttribute(mxfp_product_kernel<CG, SPLIT>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kSmemBytes) != cudaSuccess)
+      return FQ_ERR_CUDA;
+    int n = sms;
+    if (CG == 2) {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2));
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = kSmemBytes;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 2;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      int most = 0;
+      if (cudaOccupancyMaxActiveClusters(&most, mxfp_product_kernel<CG, SPLIT>, &cfg) !=
+              cudaSuccess ||
+          most < 1)
+        return FQ_ERR_CUDA;
+      n = std::min(sms / 2, most);
+    }
+    it = fit.emplace(dev, n).first;
+  }
+  room = it->second;
+  return FQ_OK;
+}
+
+template <int CG, bool SPLIT>
 fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProdArgs& a, int sms,
                          cudaStream_t s) {
-  static std::mutex mu;
-  static std::map<int, bool> done;
-  {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!done[dev]) {
-      if (cudaFuncSetAttribute(mxfp_product_kernel<SPLIT>,
-                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               kSmemBytes) != cudaSuccess)
-        return FQ_ERR_CUDA;
-      done[dev] = true;
-    }
-  }
-  const int grid = SPLIT ? a.units * a.KS : std::min(a.units, sms);
-  return launch(mxfp_product_kernel<SPLIT>, grid, kThreads, kSmemBytes, SPLIT ? a.KS : 1, s, mw, mx,
-                a) == cudaSuccess
+  int room = 0;
+  if (const fq_status st = prepare_product<CG, SPLIT>(sms, room)) return st;
+  const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room) * CG;
+  return launch(mxfp_product_kernel<CG, SPLIT>, dim3(static_cast<unsigned>(grid)), kThreads,
+                kSmemBytes, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
@@ -557,24 +672,28 @@ fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, 
   a.R = W.rows;
   a.M = X.rows;
   a.bn = pick_bn(a.M);
-  a.RT = static_cast<int>(ceil_div(a.R, kBM));
   a.TT = static_cast<int>(ceil_div(a.M, a.bn));
+  // pairs of CTAs once their tiles fill the SMs
+  const int cg = ceil_div(a.R, 2 * kBM) * a.TT >= sms / 2 ? 2 : 1;
+  a.RT = static_cast<int>(ceil_div(a.R, cg * kBM));
   a.KB = stages_of(W.cols);
   a.units = a.RT * a.TT;
   a.KS = 1;
-  while (a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
+  while (cg == 1 && a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
   a.kbs = static_cast<int>(ceil_div(a.KB, a.KS));
   a.sw = W.scales;
   a.sx = X.scales;
+  a.wgroups = static_cast<int>(ceil_div(a.R, 128));
   a.xgroups = static_cast<int>(ceil_div(a.M, 128));
   a.early_w = early_w;
   a.y = static_cast<__nv_bfloat16*>(y);
   a.status = status;
   CUtensorMap mw, mx;
-  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM) || !make_tmap(&mx, X.codes, X.rows, X.cols, a.bn))
+  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM) || !make_tmap(&mx, X.codes, X.rows, X.cols, a.bn / cg))
     return FQ_ERR_CUDA;
-  return a.KS > 1 ? launch_product<true>(mw, mx, a, sms, s)
-                  : launch_product<false>(mw, mx, a, sms, s);
+  if (cg == 2) return launch_product<2, false>(mw, mx, a, sms, s);
+  return a.KS > 1 ? launch_product<1, true>(mw, mx, a, sms, s)
+                  : launch_product<1, false>(mw, mx, a, sms, s);
 }
 
 struct Ws {
@@ -613,7 +732,7 @@ fq_status fq_mxfp_quantize(const void* x, int rows, int cols, const fq_mxfp* q,
   if (!aligned16(x)) return FQ_ERR_ALIGNMENT;
   int sms = 0;
   if (const fq_status st = check_device(sms)) return st;
-  return quantize(x, *q, sms, reinterpret_cast<cudaStream_t>(stream));
+  return quantize(x, *q, reinterpret_cast<cudaStream_t>(stream));
 }
 
 fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream) {
@@ -622,11 +741,11 @@ fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream) {
   if (!aligned16(y)) return FQ_ERR_ALIGNMENT;
   int sms = 0;
   if (const fq_status st = check_device(sms)) return st;
-  const int64_t n = static_cast<int64_t>(q->rows) * (q->cols / 8);
-  return launch(mxfp_dequantize_kernel, std::min<int64_t>(ceil_div(n, kQThreads), 16ll * sms),
-                kQThreads, 0, 1, reinterpret_cast<cudaStream_t>(stream),
+  const int KB = stages_of(q->cols);
+  return launch(mxfp_dequantize_kernel, q_grid(q->rows, KB), kQThreads, 0, 1,
+                reinterpret_cast<cudaStream_t>(stream),
                 reinterpret_cast<const uint32_t*>(q->codes),
-                static_cast<const uint8_t*>(q->scales), q->rows, q->cols, stages_of(q->cols),
+                static_cast<const uint8_t*>(q->scales), q->rows, q->cols, KB,
                 static_cast<uint4*>(y)) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
@@ -664,7 +783,7 @@ fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void*
   auto* w = static_cast<uint8_t*>(ws);
   const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
   auto s = reinterpret_cast<cudaStream_t>(stream);
-  if (const fq_status st = quantize(x, X, sms, s)) return st;
+  if (const fq_status st = quantize(x, X, s)) return st;
   return product(X, *W, y, static_cast<int32_t*>(ws), sms, true, s);
 }
 
