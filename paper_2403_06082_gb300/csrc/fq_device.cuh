@@ -342,6 +342,26 @@ __device__ __forceinline__ void umma_commit_cg(uint64_t* bar) {
   }
 }
 
+// One lane of a converged warp, the same one every time.  A role's loop runs on the whole warp and
+// only the asynchronous instructions sit behind this: their operands are then uniform values,
+// which a loop behind `lane == 0` has to move over one by one (a stage of four block-scaled MMAs
+// took 835 cycles that way, 384 of them the MMAs').
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "elect.sync _|q, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+
+// mbar_wait of a whole warp: true if it ended well for every lane.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity,
+                                               const volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+
 // ---------------------------------------------------------------------------------------------
 // gpu-scope flags
 // ---------------------------------------------------------------------------------------------

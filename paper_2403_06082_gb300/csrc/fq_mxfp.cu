@@ -4,13 +4,15 @@
 //
 // Product: y[t][i] = sum_k W[i][k] X[t][k].  A tile is CG * 128 rows of W (the accumulator's
 // rows) x bn <= 192 tokens.  Codes arrive by TMA, 256 k (128 bytes) a stage under the 128-byte
-// swizzle; scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage.  Of
-// the 512 TMEM columns two accumulators take 2 x 192 and every stage has 24 of its own for its
-// scales.
+// swizzle, in as many stages as fit shared memory: a stage's MMAs take 0.2-0.3 us and its way
+// round (copy, MMA, release) 1.5-2.  Of the 512 TMEM columns two accumulators take 2 x 192; the
+// rest is a ring of five slots of a stage's scales.
 //
-// Scales go from shared memory into TMEM by four warps with tcgen05.st.  tcgen05.cp, issued
-// between the MMAs, takes its turn in their pipe: six copies a stage made 725 cycles of the 384
-// that the stage's four MMAs of 128 x 192 x 64 take, the stores none.
+// Scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage.  Four warps
+// load them to registers three stages ahead and store them to TMEM (tcgen05.st).  The other ways
+// cost more: tcgen05.cp, issued between the MMAs, takes its turn in their pipe (six copies a
+// stage made 725 cycles of the 384 that four MMAs of 128 x 192 x 64 take, the stores none), and
+// fetching them to shared memory by bulk copies of 1 KiB kept the producer at 645 ns a stage.
 //
 // With CG = 2 a cluster of two CTAs works on 256 x bn: each stages its 128 rows of W and half of
 // the tokens' codes, one MMA reads both CTAs' shared memory.  At four times the bf16 rate the
@@ -42,30 +44,33 @@ constexpr int kBN = 192;                        // tokens per tile, at most
 constexpr int kKStage = 256;                    // k per stage: 128 bytes of codes a row
 constexpr int kABytes = kBM * kKStage / 2;
 constexpr int kSfBytes = 1024;                  // scales of 128 rows x 256 k
-constexpr int kStageSf = 3 * kSfBytes;          // W's, and up to two row groups of X's
-constexpr int kStages = 5;
+constexpr int kMaxStages = 12;
 constexpr int kThreads = 448;
 constexpr int kTmemCols = 512;
-constexpr int kSfCol = 2 * kBN;                 // TMEM columns of the scales, 24 a stage
+constexpr int kSfCol = 2 * kBN;                 // TMEM columns of the scales, 24 a slot
 constexpr int kSfCols = 24;
-static_assert(kSfCol + kStages * kSfCols <= kTmemCols, "tensor memory");
+constexpr int kSlots = 5;
+constexpr int kAhead = 3;                       // stages that the scale warps load ahead
+static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 
-constexpr int kBBytes = kBN * kKStage / 2;      // CG = 1; a CTA of a pair uses half of it
+constexpr int kNumBars = 2 * kMaxStages + 2 * kSlots + 4;
+constexpr int kTailBytes = kNumBars * 8 + 16;
+constexpr int kSmemMost = 227 * 1024;
 
-constexpr int oA = 0;
-constexpr int oB = oA + kStages * kABytes;
-constexpr int oSf = oB + kStages * kBBytes;
-constexpr int oBar = oSf + kStages * kStageSf;
-constexpr int oMisc = oBar + (4 * kStages + 4) * 8;
-constexpr int kSmemBytes = oMisc + 16 + 1024;   // + alignment slack
-static_assert(kSmemBytes <= 227 * 1024, "shared memory");
-static_assert(kBN * kBM * 4 <= oBar, "a tile's fp32 part fits the stages");
+// Shared memory: p.stages x (codes of 128 rows of W, codes of this CTA's tokens), barriers.
+__host__ __device__ constexpr int stage_bytes(int bn_cta) {
+  return kABytes + bn_cta * (kKStage / 2);
+}
+int stages_for(int bn_cta) {
+  return std::min(kMaxStages, (kSmemMost - kTailBytes - 1024) / stage_bytes(bn_cta));
+}
 
 struct ProdArgs {
   int R, M;                   // rows of W, tokens
   int bn;                     // tokens per tile
   int RT, TT, KB, KS, kbs;    // tiles of W, of tokens, stages of k, and the split of k
-  int units;                  // tiles (KS == 1)
+  int units;                  // tiles
+  int stages, stage_bytes;    // ring of code stages
   const uint8_t* sw;          // scales of W, of X: 1 KiB per row group and stage
   const uint8_t* sx;
   int wgroups, xgroups;       // row groups of W's and of X's scales
@@ -74,10 +79,9 @@ struct ProdArgs {
   int32_t* status;
 };
 
-// 512 bytes of scales (128 rows x 4, 16 bytes to the four rows l, l + 32, ...) -> 4 TMEM columns
-// of this warp's lane quarter.
-__device__ __forceinline__ void sf_store(uint32_t tmem, const uint8_t* src, int lane) {
-  const uint4 v = *reinterpret_cast<const uint4*>(src + lane * 16);
+// A lane's 16 bytes of 512 bytes of scales (rows l, l + 32, l + 64, l + 96, four each) -> 4 TMEM
+// columns of this warp's lane quarter.
+__device__ __forceinline__ void sf_store(uint32_t tmem, const uint4& v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem),
                "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
@@ -127,13 +131,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + oBar);   // codes of both CTAs (first CTA's)
-  uint64_t* empty = full + kStages;
-  uint64_t* sfull = empty + kStages;                           // this CTA's scales in smem
-  uint64_t* sready = sfull + kStages;                          // scales in TMEM (first CTA's)
-  uint64_t* tfull = sready + kStages;
-  uint64_t* tempty = tfull + 2;                                // used in the pair's first CTA
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + oMisc);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.stages * p.stage_bytes);
+  // full: codes of both CTAs have landed (first CTA's); empty: they have been read
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* sready = empty + kMaxStages;          // scales of both CTAs in TMEM (first CTA's)
+  uint64_t* sfree = sready + kSlots;              // they have been read
+  uint64_t* tfull = sfree + kSlots;
+  uint64_t* tempty = tfull + 2;                   // used in the pair's first CTA
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + kNumBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -151,11 +156,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto groups_of = [&](int n0) { return min(p.xgroups, (n0 + p.bn + 127) / 128) - n0 / 128; };
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < p.stages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
-      mbar_init(&sfull[s], 1);
+    }
+    for (int s = 0; s < kSlots; ++s) {
       mbar_init(&sready[s], 4 * CG);
+      mbar_init(&sfree[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
@@ -186,135 +193,161 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp == 0) {
     // ---------------------------------------------------------------- producer
-    if (lane == 0) {
-      const uint64_t pol_x = policy_evict_last();
-      const uint64_t pol_w = p.TT == 1 ? policy_evict_first() : pol_x;
-      const int bn_cta = p.bn / CG;
-      const uint32_t bytes = static_cast<uint32_t>(kABytes + bn_cta * (kKStage / 2));
-      auto load = [&](uint8_t* dst, const CUtensorMap* tm, int st, int x, int y, uint64_t pol) {
-        if (CG == 2) tma_load_2d_pair(dst, tm, mapa(smem_u32(&full[st]), 0), x, y, pol);
-        else tma_load_2d(dst, tm, &full[st], x, y, pol);
-      };
-      auto expect = [&](int st, int groups) {
-        // the first CTA expects the codes of both (the other's may arrive before)
-        if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&full[st], CG * bytes);
-        mbar_arrive_expect_tx(&sfull[st], static_cast<uint32_t>((1 + groups) * kSfBytes));
-      };
-      auto load_w = [&](int st, int u, int kb) {
-        const int rg = tile_rg(u);
-        load(smem + oA + st * kABytes, &tmW, st, kb * (kKStage / 2), rg * kBM, pol_w);
-        // a pair's second half may lie beyond the last row group: its rows are not used
-        bulk_load(smem + oSf + st * kStageSf,
-                  p.sw + (static_cast<int64_t>(min(rg, p.wgroups - 1)) * p.KB + kb) * kSfBytes,
-                  kSfBytes, &sfull[st], pol_w);
-      };
-      auto load_x = [&](int st, int n0, int groups, int kb) {
-        load(smem + oB + st * kBBytes, &tmX, st, kb * (kKStage / 2),
-             n0 + (CG == 2 ? rank * bn_cta : 0), pol_x);
-        for (int g = 0; g < groups; ++g)
-          bulk_load(smem + oSf + st * kStageSf + (1 + g) * kSfBytes,
-                    p.sx + (static_cast<int64_t>(n0 / 128 + g) * p.KB + kb) * kSfBytes, kSfBytes,
-                    &sfull[st], pol_x);
-      };
-      int pre = 0;
-      if (p.early_w && first < p.units) {
-        pre = min(kStages, k1 - k0);
-        for (int i = 0; i < pre; ++i) {
-          expect(i, groups_of(tile_n0(first)));
-          load_w(i, first, k0 + i);
+    const uint64_t pol_x = policy_evict_last();
+    const uint64_t pol_w = p.TT == 1 ? policy_evict_first() : pol_x;
+    const int bn_cta = p.bn / CG;
+    const uint32_t bytes = static_cast<uint32_t>(kABytes + bn_cta * (kKStage / 2));
+    // the pair's copies count on the first CTA's barriers
+    const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
+    auto load = [&](uint8_t* dst, const CUtensorMap* tm, int st, int x, int y, uint64_t pol) {
+      if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, y, pol);
+      else tma_load_2d(dst, tm, &full[st], x, y, pol);
+    };
+    auto load_w = [&](int st, int u, int kb) {
+      // the first CTA expects the codes of both (the other's may arrive before)
+      if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&full[st], CG * bytes);
+      load(smem + st * p.stage_bytes, &tmW, st, kb * (kKStage / 2), tile_rg(u) * kBM, pol_w);
+    };
+    auto load_x = [&](int st, int u, int kb) {
+      load(smem + st * p.stage_bytes + kABytes, &tmX, st, kb * (kKStage / 2),
+           tile_n0(u) + (CG == 2 ? rank * bn_cta : 0), pol_x);
+    };
+    int pre = 0;
+    if (p.early_w && first < p.units) {
+      pre = min(p.stages, k1 - k0);
+      if (elect_one())
+        for (int i = 0; i < pre; ++i) load_w(i, first, k0 + i);
+      __syncwarp();
+    }
+    pdl_wait();
+    if (p.status && blockIdx.x == 0 && lane == 0) *p.status = 0;
+    __syncwarp();
+    int stage = 0;
+    uint32_t phase = 0;
+    int64_t it = 0;
+    bool ok = true;
+    for (int u = first; ok && u < p.units; u += step) {
+      for (int kb = k0; kb < k1; ++kb, ++it) {
+        if (it >= pre) {
+          ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
+          if (!ok) break;
         }
-      }
-      pdl_wait();
-      if (p.status && blockIdx.x == 0) *p.status = 0;
-      int stage = 0;
-      uint32_t phase = 0;
-      int64_t it = 0;
-      for (int u = first; u < p.units && !*abort_flag; u += step) {
-        const int n0 = tile_n0(u), groups = groups_of(n0);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          if (it >= pre) {
-            if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
-              timed_out();
-              break;
-            }
-            expect(stage, groups);
-            load_w(stage, u, kb);
-          }
-          load_x(stage, n0, groups, kb);
-          if (++stage == kStages) stage = 0, phase ^= 1;
+        if (elect_one()) {
+          if (it >= pre) load_w(stage, u, kb);
+          load_x(stage, u, kb);
         }
+        if (++stage == p.stages) stage = 0, phase ^= 1;
       }
-      // never leave with copies in flight: wait (bounded) for the release of every stage used
-      for (int s = 0; s < kStages; ++s) {
-        const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
-        if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
-          report(p.status, FQ_ERR_TIMEOUT);
-      }
+    }
+    if (!ok) timed_out();
+    // never leave with copies in flight: wait (bounded) for the release of every stage used
+    for (int s = 0; s < p.stages; ++s) {
+      const int64_t uses = it / p.stages + (s < it % p.stages ? 1 : 0);
+      if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
+        report(p.status, FQ_ERR_TIMEOUT);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0 && (CG == 1 || rank == 0)) {
+    if (CG == 1 || rank == 0) {
       const uint32_t id0 = idesc_mxf4(CG * kBM, static_cast<uint32_t>(p.bn), 0);
       const uint32_t id2 = idesc_mxf4(CG * kBM, static_cast<uint32_t>(p.bn), 2);
-      int stage = 0, buf = 0;
-      uint32_t phase = 0, acc_phase = 0;
+      const uint64_t desc0 = umma_desc_sw128(smem_u32(smem));
+      int stage = 0, slot = 0, buf = 0;
+      uint32_t phase = 0, sphase = 0, acc_phase = 0;
       bool ok = true;
-      for (int u = first; ok && k0 < k1 && u < p.units && !*abort_flag; u += step) {
-        ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
+      for (int u = first; ok && k0 < k1 && u < p.units; u += step) {
+        ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
         // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
         const uint32_t shift = 8 + static_cast<uint32_t>(tile_n0(u) % 128) / 32;
         for (int kb = k0; kb < k1; ++kb) {
-          ok = mbar_wait(&full[stage], phase, abort_flag) &&
-               mbar_wait(&sready[stage], phase, abort_flag);
+          ok = mbar_wait_warp(&sready[slot], sphase, abort_flag) &&
+               mbar_wait_warp(&full[stage], phase, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + stage * kSfCols);
-          const uint64_t ad = umma_desc_sw128(smem_u32(smem + oA + stage * kABytes));
-          const uint64_t bd = umma_desc_sw128(smem_u32(smem + oB + stage * kBBytes));
+          const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + slot * kSfCols);
+          const uint64_t ad = desc0 + static_cast<uint32_t>(stage * p.stage_bytes >> 4);
+          const uint64_t bd = ad + (kABytes >> 4);
+          if (elect_one()) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)          // 64 k = 32 bytes along a row per step
-            umma_mxf4<CG>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
-                          tsf + shift + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
-          umma_commit_cg<CG>(&empty[stage]);
-          if (++stage == kStages) stage = 0, phase ^= 1;
+            for (int j = 0; j < 4; ++j)        // 64 k = 32 bytes along a row per step
+              umma_mxf4<CG>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
+                            tsf + shift + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
+            umma_commit_cg<CG>(&empty[stage]);
+            umma_commit_cg<CG>(&sfree[slot]);
+          }
+          if (++stage == p.stages) stage = 0, phase ^= 1;
+          if (++slot == kSlots) slot = 0, sphase ^= 1;
         }
         if (!ok) break;
-        umma_commit_cg<CG>(&tfull[buf]);
+        if (elect_one()) umma_commit_cg<CG>(&tfull[buf]);
         if (++buf == 2) buf = 0, acc_phase ^= 1;
       }
       if (!ok) timed_out();
     }
   } else if (warp >= 10) {
     // ---------------------------------------------------------------- scales
-    // A stage's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).  Its last MMAs
-    // are done once its next copies have been issued, so sfull covers them too.
+    // A slot's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).
     const uint32_t t_sf = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kSfCol;
-    int stage = 0;
-    uint32_t phase = 0;
+    struct Place {
+      int u, kb;
+    };
+    auto advance = [&](Place& q) {
+      if (++q.kb >= k1) q.kb = k0, q.u += step;
+    };
+    uint4 v[kAhead][6];
+    auto fetch = [&](const Place& q, uint4 (&r)[6]) {
+      if (q.u >= p.units || k0 >= k1) return;
+      // a pair's second half may lie beyond the last row group: its rows are not used
+      const int rg = min(tile_rg(q.u), p.wgroups - 1), n0 = tile_n0(q.u);
+      const uint8_t* w = p.sw + (static_cast<int64_t>(rg) * p.KB + q.kb) * kSfBytes + lane * 16;
+      const uint8_t* x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
+      const bool two = groups_of(n0) > 1;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        r[a] = __ldcg(reinterpret_cast<const uint4*>(w + a * 512));
+        r[2 + a] = __ldcg(reinterpret_cast<const uint4*>(x + a * 512));
+        if (two)
+          r[4 + a] = __ldcg(reinterpret_cast<const uint4*>(
+              x + static_cast<int64_t>(p.KB) * kSfBytes + a * 512));
+      }
+    };
+    pdl_wait();
+    Place now{first, k0}, then{first, k0};
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      fetch(then, v[i]);
+      advance(then);
+    }
+    int slot = 0;
+    uint32_t sphase = 0;
     bool ok = true;
-    for (int u = first; ok && u < p.units; u += step) {
-      const int groups = groups_of(tile_n0(u));
-      for (int kb = k0; kb < k1; ++kb) {
+    while (ok && k0 < k1 && now.u < p.units) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (!ok || now.u >= p.units) break;
         // the warp leaves as one: the TMEM stores are warp-wide
-        ok = __all_sync(0xffffffffu, mbar_wait(&sfull[stage], phase, abort_flag));
+        ok = __all_sync(0xffffffffu, mbar_wait(&sfree[slot], sphase ^ 1, abort_flag));
         if (!ok) break;
         tc_fence_after_sync();
-        const uint8_t* sf = smem + oSf + stage * kStageSf;
-        const uint32_t t = t_sf + static_cast<uint32_t>(stage * kSfCols);
+        const uint32_t t = t_sf + static_cast<uint32_t>(slot * kSfCols);
+        const bool two = groups_of(tile_n0(now.u)) > 1;
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-          sf_store(t + a * 4, sf + a * 512, lane);
-          for (int g = 0; g < groups; ++g)
-            sf_store(t + 8 + a * 8 + g * 4, sf + (1 + g) * kSfBytes + a * 512, lane);
+          sf_store(t + a * 4, v[i][a]);
+          sf_store(t + 8 + a * 8, v[i][2 + a]);
+          if (two) sf_store(t + 12 + a * 8, v[i][4 + a]);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) arrive_first(&sready[stage]);
-        if (++stage == kStages) stage = 0, phase ^= 1;
+        if (lane == 0) arrive_first(&sready[slot]);
+        if (++slot == kSlots) slot = 0, sphase ^= 1;
+        fetch(then, v[i]);
+        advance(then);
+        advance(now);
       }
     }
     if (!ok) timed_out();
@@ -618,14 +651,14 @@ fq_status prepare_product(int sms, int& room) {
   if (it == fit.end()) {
     if (cudaFuncSetAttribute(mxfp_product_kernel<CG, SPLIT>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             kSmemBytes) != cudaSuccess)
+                             kSmemMost) != cudaSuccess)
       return FQ_ERR_CUDA;
     int n = sms;
     if (CG == 2) {
       cudaLaunchConfig_t cfg{};
       cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2));
       cfg.blockDim = dim3(kThreads);
-      cfg.dynamicSmemBytes = kSmemBytes;
+      cfg.dynamicSmemBytes = kSmemMost;
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = 2;
@@ -653,7 +686,7 @@ fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const Pro
   if (const fq_status st = prepare_product<CG, SPLIT>(sms, room)) return st;
   const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room) * CG;
   return launch(mxfp_product_kernel<CG, SPLIT>, dim3(static_cast<unsigned>(grid)), kThreads,
-                kSmemBytes, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
+                static_cast<size_t>(a.stages) * a.stage_bytes + kTailBytes + 1024, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
@@ -681,6 +714,8 @@ fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, 
   a.KS = 1;
   while (cg == 1 && a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
   a.kbs = static_cast<int>(ceil_div(a.KB, a.KS));
+  a.stages = stages_for(a.bn / cg);
+  a.stage_bytes = stage_bytes(a.bn / cg);
   a.sw = W.scales;
   a.sx = X.scales;
   a.wgroups = static_cast<int>(ceil_div(a.R, 128));
