@@ -203,20 +203,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, y, pol);
       else tma_load_2d(dst, tm, &full[st], x, y, pol);
     };
-    auto load_w = [&](int st, int u, int kb) {
+    // coordinates of a tile; what a stage's copies need is kept out of divisions (with them the
+    // producer took 700 cycles a stage)
+    auto w_row = [&](int u) { return tile_rg(u) * kBM; };
+    auto x_row = [&](int u) { return tile_n0(u) + (CG == 2 ? rank * bn_cta : 0); };
+    auto load_w = [&](int st, uint8_t* dst, int row, int x) {
       // the first CTA expects the codes of both (the other's may arrive before)
       if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&full[st], CG * bytes);
-      load(smem + st * p.stage_bytes, &tmW, st, kb * (kKStage / 2), tile_rg(u) * kBM, pol_w);
+      load(dst, &tmW, st, x, row, pol_w);
     };
-    auto load_x = [&](int st, int u, int kb) {
-      load(smem + st * p.stage_bytes + kABytes, &tmX, st, kb * (kKStage / 2),
-           tile_n0(u) + (CG == 2 ? rank * bn_cta : 0), pol_x);
+    auto load_x = [&](int st, uint8_t* dst, int row, int x) {
+      load(dst + kABytes, &tmX, st, x, row, pol_x);
     };
     int pre = 0;
     if (p.early_w && first < p.units) {
       pre = min(p.stages, k1 - k0);
+      const int row = w_row(first);
       if (elect_one())
-        for (int i = 0; i < pre; ++i) load_w(i, first, k0 + i);
+        for (int i = 0; i < pre; ++i)
+          load_w(i, smem + i * p.stage_bytes, row, (k0 + i) * (kKStage / 2));
       __syncwarp();
     }
     pdl_wait();
@@ -226,17 +231,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t phase = 0;
     int64_t it = 0;
     bool ok = true;
+    uint8_t* dst = smem;
     for (int u = first; ok && u < p.units; u += step) {
-      for (int kb = k0; kb < k1; ++kb, ++it) {
-        if (it >= pre) {
+      const int wr = w_row(u), xr = x_row(u);
+      int x = k0 * (kKStage / 2);
+      for (int kb = k0; kb < k1; ++kb, ++it, x += kKStage / 2) {
+        const bool early = it < pre;
+        if (!early) {
           ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
           if (!ok) break;
         }
         if (elect_one()) {
-          if (it >= pre) load_w(stage, u, kb);
-          load_x(stage, u, kb);
+          if (!early) load_w(stage, dst, wr, x);
+          load_x(stage, dst, xr, x);
         }
-        if (++stage == p.stages) stage = 0, phase ^= 1;
+        dst += p.stage_bytes;
+        if (++stage == p.stages) stage = 0, phase ^= 1, dst = smem;
       }
     }
     if (!ok) timed_out();
@@ -291,63 +301,74 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- scales
     // A slot's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).
     const uint32_t t_sf = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kSfCol;
-    struct Place {
+    // The stages to come, walked by pointers: divisions only where a tile begins.
+    struct Walk {
       int u, kb;
-    };
-    auto advance = [&](Place& q) {
-      if (++q.kb >= k1) q.kb = k0, q.u += step;
-    };
-    uint4 v[kAhead][6];
-    auto fetch = [&](const Place& q, uint4 (&r)[6]) {
-      if (q.u >= p.units || k0 >= k1) return;
+      const uint8_t *w, *x;
+      bool two;
+    } q{first, k0, nullptr, nullptr, false};
+    auto enter = [&]() {
+      if (q.u >= p.units) return;
       // a pair's second half may lie beyond the last row group: its rows are not used
       const int rg = min(tile_rg(q.u), p.wgroups - 1), n0 = tile_n0(q.u);
-      const uint8_t* w = p.sw + (static_cast<int64_t>(rg) * p.KB + q.kb) * kSfBytes + lane * 16;
-      const uint8_t* x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
-      const bool two = groups_of(n0) > 1;
+      q.w = p.sw + (static_cast<int64_t>(rg) * p.KB + q.kb) * kSfBytes + lane * 16;
+      q.x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
+      q.two = groups_of(n0) > 1;
+    };
+    const int64_t next_group = static_cast<int64_t>(p.KB) * kSfBytes;
+    struct Held {
+      uint4 v[6];
+      bool any, two;
+    } held[kAhead];
+    auto fetch = [&](Held& h) {
+      h.any = k0 < k1 && q.u < p.units;
+      if (!h.any) return;
+      h.two = q.two;
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
-        r[a] = __ldcg(reinterpret_cast<const uint4*>(w + a * 512));
-        r[2 + a] = __ldcg(reinterpret_cast<const uint4*>(x + a * 512));
-        if (two)
-          r[4 + a] = __ldcg(reinterpret_cast<const uint4*>(
-              x + static_cast<int64_t>(p.KB) * kSfBytes + a * 512));
+        h.v[a] = __ldcg(reinterpret_cast<const uint4*>(q.w + a * 512));
+        h.v[2 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + a * 512));
+        if (q.two) h.v[4 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + next_group + a * 512));
+      }
+      if (++q.kb < k1) {
+        q.w += kSfBytes;
+        q.x += kSfBytes;
+      } else {
+        q.kb = k0;
+        q.u += step;
+        enter();
       }
     };
     pdl_wait();
-    Place now{first, k0}, then{first, k0};
+    enter();
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      fetch(then, v[i]);
-      advance(then);
-    }
+    for (int i = 0; i < kAhead; ++i) fetch(held[i]);
     int slot = 0;
     uint32_t sphase = 0;
-    bool ok = true;
-    while (ok && k0 < k1 && now.u < p.units) {
+    bool ok = true, more = true;
+    while (more) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        if (!ok || now.u >= p.units) break;
+        more = more && held[i].any;
+        if (!more) break;
         // the warp leaves as one: the TMEM stores are warp-wide
-        ok = __all_sync(0xffffffffu, mbar_wait(&sfree[slot], sphase ^ 1, abort_flag));
+        ok = mbar_wait_warp(&sfree[slot], sphase ^ 1, abort_flag);
+        more = ok;
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t t = t_sf + static_cast<uint32_t>(slot * kSfCols);
-        const bool two = groups_of(tile_n0(now.u)) > 1;
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-          sf_store(t + a * 4, v[i][a]);
-          sf_store(t + 8 + a * 8, v[i][2 + a]);
-          if (two) sf_store(t + 12 + a * 8, v[i][4 + a]);
+          sf_store(t + a * 4, held[i].v[a]);
+          sf_store(t + 8 + a * 8, held[i].v[2 + a]);
+          if (held[i].two) sf_store(t + 12 + a * 8, held[i].v[4 + a]);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) arrive_first(&sready[slot]);
         if (++slot == kSlots) slot = 0, sphase ^= 1;
-        fetch(then, v[i]);
-        advance(then);
-        advance(now);
+        fetch(held[i]);
       }
     }
     if (!ok) timed_out();
