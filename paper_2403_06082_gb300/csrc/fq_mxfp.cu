@@ -8,11 +8,17 @@
 // round (copy, MMA, release) 1.5-2.  Of the 512 TMEM columns two accumulators take 2 x 192; the
 // rest is a ring of five slots of a stage's scales.
 //
-// Scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage.  Four warps
-// load them to registers three stages ahead and store them to TMEM (tcgen05.st).  The other ways
-// cost more: tcgen05.cp, issued between the MMAs, takes its turn in their pipe (six copies a
-// stage made 725 cycles of the 384 that four MMAs of 128 x 192 x 64 take, the stores none), and
-// fetching them to shared memory by bulk copies of 1 KiB kept the producer at 645 ns a stage.
+// Scales lie in memory as the tensor cores want them, 1 KiB per 128 rows and stage.  Two groups of
+// four warps load every other stage's to registers ahead of time and store them to TMEM
+// (tcgen05.st).  The other ways cost more: tcgen05.cp, issued between the MMAs, takes its turn in
+// their pipe (six copies a stage made 725 cycles of the 384 that four MMAs of 128 x 192 x 64 take,
+// the stores none), and fetching them to shared memory by bulk copies of 1 KiB kept the producer
+// at 645 ns a stage.
+//
+// A stage is 384 cycles of MMA, and every role has to keep up with that: its loop runs on a whole
+// warp, without divisions, and waits for one barrier a stage (about 110 cycles even when it is
+// there): codes and scales count on the same one, and a slot of scales is free when the stage that
+// used it is.  W's and X's codes have a producer each.
 //
 // With CG = 2 a cluster of two CTAs works on 256 x bn: each stages its 128 rows of W and half of
 // the tokens' codes, one MMA reads both CTAs' shared memory.  At four times the bf16 rate the
@@ -22,9 +28,9 @@
 // KS CTAs splits the k range of one tile and adds the parts up, in rank order, through
 // distributed shared memory.
 //
-// Warp roles: warp 0 producer (one lane), warp 1 TMEM owner + MMA issuer (one lane, of the first
-// CTA of a pair), warps 2-9 epilogue (thread = accumulator row, half of the tokens), warps 10-13
-// scales.
+// Warp roles: warp 0 producer of W's codes, warp 1 TMEM owner + MMA issuer (of the first CTA of a
+// pair), warps 2-9 epilogue (thread = accumulator row, half of the tokens), warps 10-17 scales,
+// warp 18 producer of X's codes.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -45,15 +51,15 @@ constexpr int kKStage = 256;                    // k per stage: 128 bytes of cod
 constexpr int kABytes = kBM * kKStage / 2;
 constexpr int kSfBytes = 1024;                  // scales of 128 rows x 256 k
 constexpr int kMaxStages = 12;
-constexpr int kThreads = 448;
+constexpr int kThreads = 608;
 constexpr int kTmemCols = 512;
 constexpr int kSfCol = 2 * kBN;                 // TMEM columns of the scales, 24 a slot
 constexpr int kSfCols = 24;
 constexpr int kSlots = 5;
-constexpr int kAhead = 3;                       // stages that the scale warps load ahead
+constexpr int kAhead = 2;                       // of its stages that a group of scale warps holds
 static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 
-constexpr int kNumBars = 2 * kMaxStages + 2 * kSlots + 4;
+constexpr int kNumBars = 2 * kMaxStages + 4;
 constexpr int kTailBytes = kNumBars * 8 + 16;
 constexpr int kSmemMost = 227 * 1024;
 
@@ -62,6 +68,7 @@ __host__ __device__ constexpr int stage_bytes(int bn_cta) {
   return kABytes + bn_cta * (kKStage / 2);
 }
 int stages_for(int bn_cta) {
+  // at least kSlots: a slot of scales then never waits for a later round of its stage
   return std::min(kMaxStages, (kSmemMost - kTailBytes - 1024) / stage_bytes(bn_cta));
 }
 
@@ -132,16 +139,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.stages * p.stage_bytes);
-  // full: codes of both CTAs have landed (first CTA's); empty: they have been read
+  // full: codes of both CTAs in shared memory, scales of both in TMEM (first CTA's barriers);
+  // empty: they have been read
   uint64_t* empty = full + kMaxStages;
-  uint64_t* sready = empty + kMaxStages;          // scales of both CTAs in TMEM (first CTA's)
-  uint64_t* sfree = sready + kSlots;              // they have been read
-  uint64_t* tfull = sfree + kSlots;
+  uint64_t* tfull = empty + kMaxStages;
   uint64_t* tempty = tfull + 2;                   // used in the pair's first CTA
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + kNumBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
   // SPLIT: one tile per cluster, its k range over the ranks; else tiles in turn
   const int rank = SPLIT || CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
   const int first = static_cast<int>(blockIdx.x) / (SPLIT ? p.KS : CG);
@@ -157,12 +164,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], 1 + 4 * CG);
       mbar_init(&empty[s], 1);
-    }
-    for (int s = 0; s < kSlots; ++s) {
-      mbar_init(&sready[s], 4 * CG);
-      mbar_init(&sfree[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&tfull[b], 1);
@@ -191,62 +194,54 @@ __global__ void __launch_bounds__(kThreads, 1)
     *abort_flag = 1;
   };
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- producer
-    const uint64_t pol_x = policy_evict_last();
-    const uint64_t pol_w = p.TT == 1 ? policy_evict_first() : pol_x;
+  if (warp == 0 || warp == 18) {
+    // ---------------------------------------------------------------- producers
+    const bool is_w = warp == 0;
+    const uint64_t pol = is_w && p.TT == 1 ? policy_evict_first() : policy_evict_last();
     const int bn_cta = p.bn / CG;
     const uint32_t bytes = static_cast<uint32_t>(kABytes + bn_cta * (kKStage / 2));
+    const CUtensorMap* tm = is_w ? &tmW : &tmX;
     // the pair's copies count on the first CTA's barriers
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
-    auto load = [&](uint8_t* dst, const CUtensorMap* tm, int st, int x, int y, uint64_t pol) {
-      if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, y, pol);
-      else tma_load_2d(dst, tm, &full[st], x, y, pol);
+    auto row_of = [&](int u) {
+      return is_w ? tile_rg(u) * kBM : tile_n0(u) + (CG == 2 ? rank * bn_cta : 0);
     };
-    // coordinates of a tile; what a stage's copies need is kept out of divisions (with them the
-    // producer took 700 cycles a stage)
-    auto w_row = [&](int u) { return tile_rg(u) * kBM; };
-    auto x_row = [&](int u) { return tile_n0(u) + (CG == 2 ? rank * bn_cta : 0); };
-    auto load_w = [&](int st, uint8_t* dst, int row, int x) {
-      // the first CTA expects the codes of both (the other's may arrive before)
-      if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&full[st], CG * bytes);
-      load(dst, &tmW, st, x, row, pol_w);
+    auto load = [&](int st, uint8_t* dst, int row, int x) {
+      // W's producer of the first CTA expects the codes of both producers and CTAs (the others'
+      // may arrive before)
+      if (is_w && (CG == 1 || rank == 0)) mbar_arrive_expect_tx(&full[st], CG * bytes);
+      if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, row, pol);
+      else tma_load_2d(dst, tm, &full[st], x, row, pol);
     };
-    auto load_x = [&](int st, uint8_t* dst, int row, int x) {
-      load(dst + kABytes, &tmX, st, x, row, pol_x);
-    };
+    uint8_t* const dst0 = smem + (is_w ? 0 : kABytes);
     int pre = 0;
-    if (p.early_w && first < p.units) {
+    if (is_w && p.early_w && first < p.units) {
       pre = min(p.stages, k1 - k0);
-      const int row = w_row(first);
+      const int row = row_of(first);
       if (elect_one())
         for (int i = 0; i < pre; ++i)
-          load_w(i, smem + i * p.stage_bytes, row, (k0 + i) * (kKStage / 2));
+          load(i, dst0 + i * p.stage_bytes, row, (k0 + i) * (kKStage / 2));
       __syncwarp();
     }
     pdl_wait();
-    if (p.status && blockIdx.x == 0 && lane == 0) *p.status = 0;
+    if (p.status && blockIdx.x == 0 && is_w && lane == 0) *p.status = 0;
     __syncwarp();
     int stage = 0;
     uint32_t phase = 0;
     int64_t it = 0;
     bool ok = true;
-    uint8_t* dst = smem;
+    uint8_t* dst = dst0;
     for (int u = first; ok && u < p.units; u += step) {
-      const int wr = w_row(u), xr = x_row(u);
+      const int row = row_of(u);
       int x = k0 * (kKStage / 2);
       for (int kb = k0; kb < k1; ++kb, ++it, x += kKStage / 2) {
-        const bool early = it < pre;
-        if (!early) {
+        if (it >= pre) {
           ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
           if (!ok) break;
-        }
-        if (elect_one()) {
-          if (!early) load_w(stage, dst, wr, x);
-          load_x(stage, dst, xr, x);
+          if (elect_one()) load(stage, dst, row, x);
         }
         dst += p.stage_bytes;
-        if (++stage == p.stages) stage = 0, phase ^= 1, dst = smem;
+        if (++stage == p.stages) stage = 0, phase ^= 1, dst = dst0;
       }
     }
     if (!ok) timed_out();
@@ -263,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t id2 = idesc_mxf4(CG * kBM, static_cast<uint32_t>(p.bn), 2);
       const uint64_t desc0 = umma_desc_sw128(smem_u32(smem));
       int stage = 0, slot = 0, buf = 0;
-      uint32_t phase = 0, sphase = 0, acc_phase = 0;
+      uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
       for (int u = first; ok && k0 < k1 && u < p.units; u += step) {
         ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
@@ -273,8 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
         const uint32_t shift = 8 + static_cast<uint32_t>(tile_n0(u) % 128) / 32;
         for (int kb = k0; kb < k1; ++kb) {
-          ok = mbar_wait_warp(&sready[slot], sphase, abort_flag) &&
-               mbar_wait_warp(&full[stage], phase, abort_flag);
+          ok = mbar_wait_warp(&full[stage], phase, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + slot * kSfCols);
@@ -286,10 +280,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               umma_mxf4<CG>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
                             tsf + shift + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
             umma_commit_cg<CG>(&empty[stage]);
-            umma_commit_cg<CG>(&sfree[slot]);
           }
           if (++stage == p.stages) stage = 0, phase ^= 1;
-          if (++slot == kSlots) slot = 0, sphase ^= 1;
+          if (++slot == kSlots) slot = 0;
         }
         if (!ok) break;
         if (elect_one()) umma_commit_cg<CG>(&tfull[buf]);
@@ -297,11 +290,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) timed_out();
     }
-  } else if (warp >= 10) {
+  } else if (warp >= 10 && warp < 18) {
     // ---------------------------------------------------------------- scales
     // A slot's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).
     const uint32_t t_sf = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + kSfCol;
-    // The stages to come, walked by pointers: divisions only where a tile begins.
+    // This group's stages (every other one), walked by pointers: divisions only where a tile
+    // begins.
+    const int group = (warp - 10) >> 2;
+    const int64_t next_group = static_cast<int64_t>(p.KB) * kSfBytes;
     struct Walk {
       int u, kb;
       const uint8_t *w, *x;
@@ -315,7 +311,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       q.x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
       q.two = groups_of(n0) > 1;
     };
-    const int64_t next_group = static_cast<int64_t>(p.KB) * kSfBytes;
+    auto skip = [&]() {
+      if (++q.kb < k1) {
+        q.w += kSfBytes;
+        q.x += kSfBytes;
+      } else {
+        q.kb = k0;
+        q.u += step;
+        enter();
+      }
+    };
     struct Held {
       uint4 v[6];
       bool any, two;
@@ -330,21 +335,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         h.v[2 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + a * 512));
         if (q.two) h.v[4 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + next_group + a * 512));
       }
-      if (++q.kb < k1) {
-        q.w += kSfBytes;
-        q.x += kSfBytes;
-      } else {
-        q.kb = k0;
-        q.u += step;
-        enter();
-      }
+      skip();
+      skip();
     };
     pdl_wait();
     enter();
+    if (group) skip();
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(held[i]);
-    int slot = 0;
-    uint32_t sphase = 0;
+    // of this group's next stage: its place in the ring, its slot, and the stage that used the
+    // slot before (kSlots stages earlier) with the parity of its release
+    int stage = group, slot = group, before = p.stages + group - kSlots;
+    uint32_t parity = 1;                           // of a phase before the first: passes
+    if (before >= p.stages) before -= p.stages, parity ^= 1;
+    const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
     bool ok = true, more = true;
     while (more) {
 #pragma unroll
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         more = more && held[i].any;
         if (!more) break;
         // the warp leaves as one: the TMEM stores are warp-wide
-        ok = mbar_wait_warp(&sfree[slot], sphase ^ 1, abort_flag);
+        ok = mbar_wait_warp(&empty[before], parity, abort_flag);
         more = ok;
         if (!ok) break;
         tc_fence_after_sync();
@@ -366,8 +370,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) arrive_first(&sready[slot]);
-        if (++slot == kSlots) slot = 0, sphase ^= 1;
+        if (lane == 0) {
+          if (CG == 2) mbar_arrive_cluster(full0 + static_cast<uint32_t>(stage) * 8);
+          else mbar_arrive(&full[stage]);
+        }
+        if ((stage += 2) >= p.stages) stage -= p.stages;
+        if ((slot += 2) >= kSlots) slot -= kSlots;
+        if ((before += 2) >= p.stages) before -= p.stages, parity ^= 1;
         fetch(held[i]);
       }
     }
@@ -714,10 +723,17 @@ fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const Pro
 
 // Tokens per tile: all of up to 192 in one tile.  More go by tiles of 128 or 192, whose first
 // token is a multiple of 64 (scales of X then start on an even column of their tile), whichever
-// wastes fewer columns, the wider of equals.
-int pick_bn(int M) {
+// takes less time: a stage took 303 ns at 128 tokens and 344 at 192 (d = 8192, pairs), so time
+// goes as the rounds of tiles over the SMs x (tokens + 345).
+int pick_bn(int M, int R, int sms) {
   if (M <= kBN) return static_cast<int>(round_up(M, 16));
-  return round_up(M, 128) < round_up(M, 192) ? 128 : 192;
+  auto cost = [&](int bn) {
+    const int64_t pairs = ceil_div(R, 2 * kBM) * ceil_div(M, bn);
+    const int64_t rounds = pairs >= sms / 2 ? ceil_div(pairs, sms / 2)
+                                            : ceil_div(ceil_div(R, kBM) * ceil_div(M, bn), sms);
+    return rounds * (bn + 345);
+  };
+  return cost(128) < cost(192) ? 128 : 192;
 }
 
 fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, int sms,
@@ -725,7 +741,7 @@ fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, 
   ProdArgs a{};
   a.R = W.rows;
   a.M = X.rows;
-  a.bn = pick_bn(a.M);
+  a.bn = pick_bn(a.M, a.R, sms);
   a.TT = static_cast<int>(ceil_div(a.M, a.bn));
   // pairs of CTAs once their tiles fill the SMs
   const int cg = ceil_div(a.R, 2 * kBM) * a.TT >= sms / 2 ? 2 : 1;
