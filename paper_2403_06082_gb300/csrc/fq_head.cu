@@ -23,8 +23,8 @@
 // what is below its accumulator's last bit at every step, so a long sum drifts towards zero: at
 // d = 4096 the loss was off by 1.9e-6 of its norm against 4e-7 for fp32 products.
 //
-// Warp roles: warp 0 TMA producer (one lane), warp 1 TMEM owner + MMA issuer (one lane, of the
-// first CTA of a pair), warps 2-9 epilogue (thread = half an accumulator row).
+// Warp roles: warp 0 producer of A, warp 1 TMEM owner + MMA issuer (of the first CTA of a pair),
+// warps 2-9 epilogue (thread = half an accumulator row), warp 10 producer of B.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -48,7 +48,7 @@ constexpr int kBN = 256;                        // accumulator columns per tile,
 constexpr int kBK = 64;                         // k per stage: one 128-byte swizzle row of bf16
 constexpr int kABytes = kBM * kBK * 2;
 constexpr int kAtomBytes = 64 * kBK * 2;        // MN-major: 64 rows of the operand x kBK
-constexpr int kThreads = 320;
+constexpr int kThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kChunk = 32;                      // accumulator columns per epilogue step
 constexpr int kMinBn = 32;
@@ -176,7 +176,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + Lo::oMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+  const int lane = threadIdx.x & 31;
   const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
   const int cid = static_cast<int>(blockIdx.x) / CG, ncl = static_cast<int>(gridDim.x) / CG;
   // unit u = (split * NT + column tile) * RT + row tile: the CTAs of a wave share the column
@@ -207,103 +208,101 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
 
-  if (warp == 0) {
-    // ---------------------------------------------------------------- TMA producer
-    if (lane == 0) {
-      pdl_wait();
-      if (p.clear && blockIdx.x == 0) *p.status = 0;
-      const uint64_t pol = policy_evict_last();
-      const int bn_cta = p.bn / CG;                 // rows of B of this CTA
-      const uint32_t bytes =
-          (a_mn_major(MODE) ? kABytes : static_cast<uint32_t>(p.a_rows) * kBK * 2) +
-          (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(bn_cta) * kBK * 2);
-      // a B that is read once (one row tile) need not stay in L2
-      const uint64_t pol_b = p.RT == 1 ? policy_evict_first() : pol;
-      int stage = 0;
-      uint32_t phase = 0;
-      int64_t it = 0;
-      for (int u = cid; u < p.units && !*abort_flag; u += ncl) {
-        const int r0 = (unit_rt(u) * CG + rank) * kBM;
-        const int n0 = unit_nt(u) * p.bn + rank * bn_cta;
-        const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag)) {
-            report(p.status, FQ_ERR_TIMEOUT);
-            *abort_flag = 1;
-            break;
-          }
-          uint8_t* a = smem + Lo::oA + stage * kABytes;
-          uint8_t* b = smem + Lo::oB + stage * kBBytes;
-          const uint32_t lead = CG == 2 ? mapa(smem_u32(&full[stage]), 0) : 0;
-          // The first CTA expects the bytes of both.  The other's may arrive before it does: the
-          // phase still waits for the one arrival.
-          if (rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
-          auto load = [&](uint8_t* dst, const CUtensorMap* tm, int cx, int cy, uint64_t pl) {
-            if (CG == 2) tma_load_2d_pair(dst, tm, lead, cx, cy, pl);
-            else tma_load_2d(dst, tm, &full[stage], cx, cy, pl);
-          };
-          if (a_mn_major(MODE)) {
-#pragma unroll
-            for (int i = 0; i < kBM / 64; ++i)
-              load(a + i * kAtomBytes, &tmA, r0 + 64 * i, kb * kBK, pol);
+  if (warp == 0 || warp == 10) {
+    // ---------------------------------------------------------------- producers
+    const bool is_a = warp == 0;
+    pdl_wait();
+    if (p.clear && blockIdx.x == 0 && is_a && lane == 0) *p.status = 0;
+    __syncwarp();
+    // a B that is read once (one row tile) need not stay in L2
+    const uint64_t pol = !is_a && p.RT == 1 ? policy_evict_first() : policy_evict_last();
+    const int bn_cta = p.bn / CG;                   // rows of B of this CTA
+    const uint32_t bytes =
+        (a_mn_major(MODE) ? kABytes : static_cast<uint32_t>(p.a_rows) * kBK * 2) +
+        (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(bn_cta) * kBK * 2);
+    const CUtensorMap* tm = is_a ? &tmA : &tmB;
+    const bool mn = is_a ? a_mn_major(MODE) : b_mn_major(MODE);
+    const int boxes = is_a ? kBM / 64 : kBN / CG / 64;           // of an MN-major operand
+    // the pair's copies count on the first CTA's barriers
+    const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
+    auto load = [&](uint8_t* dst, int st, int x, int y) {
+      if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, y, pol);
+      else tma_load_2d(dst, tm, &full[st], x, y, pol);
+    };
+    int stage = 0;
+    uint32_t phase = 0;
+    int64_t it = 0;
+    bool ok = true;
+    for (int u = cid; ok && u < p.units; u += ncl) {
+      const int row = is_a ? (unit_rt(u) * CG + rank) * kBM : unit_nt(u) * p.bn + rank * bn_cta;
+      const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
+      for (int kb = k0; kb < k1; ++kb, ++it) {
+        ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
+        if (!ok) break;
+        if (elect_one()) {
+          // A's producer of the first CTA expects the bytes of both producers and CTAs.  The
+          // others' may arrive before that: the phase still waits for the one arrival.
+          if (is_a && rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
+          uint8_t* dst = smem + (is_a ? Lo::oA + stage * kABytes : Lo::oB + stage * kBBytes);
+          if (mn) {
+            for (int i = 0; i < boxes; ++i) load(dst + i * kAtomBytes, stage, row + 64 * i, kb * kBK);
           } else {
-            load(a, &tmA, kb * kBK, r0, pol);
+            load(dst, stage, kb * kBK, row);
           }
-          if (b_mn_major(MODE)) {
-#pragma unroll
-            for (int i = 0; i < kBN / CG / 64; ++i)
-              load(b + i * kAtomBytes, &tmB, n0 + 64 * i, kb * kBK, pol_b);
-          } else {
-            load(b, &tmB, kb * kBK, n0, pol_b);
-          }
-          if (++stage == kStages) stage = 0, phase ^= 1;
         }
+        if (++stage == kStages) stage = 0, phase ^= 1;
       }
-      // Never leave with copies in flight: a stage is released once the MMAs that read its
-      // copies (of both CTAs) are done, so wait (bounded) for the release of every stage used.
-      for (int s = 0; s < kStages; ++s) {
-        const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
-        if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
-          report(p.status, FQ_ERR_TIMEOUT);
-      }
+    }
+    if (!ok) {
+      report(p.status, FQ_ERR_TIMEOUT);
+      *abort_flag = 1;
+    }
+    // Never leave with copies in flight: a stage is released once the MMAs that read its copies
+    // (of both CTAs) are done, so wait (bounded) for the release of every stage used.
+    for (int s = 0; s < kStages; ++s) {
+      const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
+      if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
+        report(p.status, FQ_ERR_TIMEOUT);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       const uint32_t idesc = umma_idesc_bf16(CG * kBM, static_cast<uint32_t>(p.bn)) |
                              (a_mn_major(MODE) ? 1u << 15 : 0u) |
                              (b_mn_major(MODE) ? 1u << 16 : 0u);
       // 16 k per MMA: 32 bytes along a K-major row, or 16 rows of 128 bytes of an MN-major tile
       constexpr uint64_t stepA = (a_mn_major(MODE) ? 2048 : 32) >> 4;
       constexpr uint64_t stepB = (b_mn_major(MODE) ? 2048 : 32) >> 4;
+      const uint32_t sa = smem_u32(smem + Lo::oA), sb = smem_u32(smem + Lo::oB);
+      const uint64_t ad0 = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
+      const uint64_t bd0 = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      for (int u = cid; ok && u < p.units && !*abort_flag; u += ncl) {
+      for (int u = cid; ok && u < p.units; u += ncl) {
         const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
         for (int ka = k0; ok && ka < k1;) {
           const int ke = MODE == kLse ? min(k1, ka + kSegBlocks) : k1;
-          ok = mbar_wait(&tempty[buf], acc_phase ^ 1, abort_flag);
+          ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
           const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
           for (int kb = ka; kb < ke; ++kb) {
-            ok = mbar_wait(&full[stage], phase, abort_flag);
+            ok = mbar_wait_warp(&full[stage], phase, abort_flag);
             if (!ok) break;
-            tc_fence_after_sync();
-            const uint32_t sa = smem_u32(smem + Lo::oA + stage * kABytes);
-            const uint32_t sb = smem_u32(smem + Lo::oB + stage * kBBytes);
-            const uint64_t ad = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
-            const uint64_t bd = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
+            const uint64_t ad = ad0 + static_cast<uint32_t>(stage * (kABytes >> 4));
+            const uint64_t bd = bd0 + static_cast<uint32_t>(stage * (kBBytes >> 4));
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < kBK / 16; ++k)
-              umma_cg<CG>(d, ad + k * stepA, bd + k * stepB, idesc,
-                          (kb > ka || k > 0) ? 1u : 0u);
-            umma_commit_cg<CG>(&empty[stage]);
+              for (int k = 0; k < kBK / 16; ++k)
+                umma_cg<CG>(d, ad + k * stepA, bd + k * stepB, idesc,
+                            (kb > ka || k > 0) ? 1u : 0u);
+              umma_commit_cg<CG>(&empty[stage]);
+            }
             if (++stage == kStages) stage = 0, phase ^= 1;
           }
           if (!ok) break;
-          umma_commit_cg<CG>(&tfull[buf]);
+          if (elect_one()) umma_commit_cg<CG>(&tfull[buf]);
           if (++buf == 2) buf = 0, acc_phase ^= 1;
           ka = ke;
         }
