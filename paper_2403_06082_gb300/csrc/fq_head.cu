@@ -3,16 +3,19 @@
 //
 // One persistent, warp-specialised kernel computes tiles of  acc[i][j] = sum_k A[i][k] B[j][k]
 // (CG * 128 rows of A on the tensor cores' rows, bn <= 256 rows of B on their columns, fp32 in
-// TMEM) for the four products of a training step:
-//   kLse  A = x (tokens),   B = W (vocabulary),  k = d: per token and tile the running maximum
-//         and sum of exponentials, and the logits of the token's targets;
-//   kDl   the same product again: ds = g (softmax - target) as bf16, one piece of the vocabulary;
-//   kDx   A = ds (tokens),  B = W^T (d columns), k = the piece: dx;
-//   kDw   A = ds^T (vocabulary rows), B = x^T (d columns), k = tokens: dW of the piece.
-// A token is a row of the accumulator, i.e. one epilogue thread per half row, so the softmax
-// statistics need no exchange between threads.  Operands whose contraction dimension is not the
-// contiguous one (W in kDx, ds and x in kDw) are read as they lie in memory, as MN-major tiles:
-// nothing is transposed.
+// TMEM) for the four products of a training step, in three modes:
+//   kLse   A = x (tokens),  B = W (vocabulary),  k = d: per token and tile the maximum and the sum
+//          of exponentials, and the logits of the token's targets;
+//   kDl    the same product again: ds = g (softmax - target) as bf16, one piece of the vocabulary;
+//   kGrad  both gradients from the piece's ds in one launch, the longer tiles first:
+//          dx  A = ds (tokens),             B = W^T (d columns), k = the piece;
+//          dW  A = ds^T (vocabulary rows),  B = x^T (d columns), k = tokens.
+// A token is a row of the accumulator in kLse and kDl, i.e. one epilogue thread per half row, so
+// the softmax statistics need no exchange between threads.  Operands whose contraction dimension
+// is not the contiguous one (W for dx, ds and x for dW) are read as they lie in memory, as
+// MN-major tiles: nothing is transposed.  ds is rounded to bf16, the type that the tensor cores
+// multiply with bf16 W and x: it adds 2^-9 of each entry, of either sign, to gradients that are
+// rounded to bf16 themselves.
 //
 // With CG = 2 a cluster of two CTAs works on one tile of 256 x bn: each CTA stages its 128 rows
 // of A and half of the rows of B, one MMA reads both CTAs' shared memory, and each CTA finishes
@@ -41,7 +44,7 @@
 namespace fq {
 namespace {
 
-enum Mode : int { kLse = 0, kDl = 1, kDx = 2, kDw = 3 };
+enum Mode : int { kLse = 0, kDl = 1, kGrad = 2 };
 
 constexpr int kBM = 128;                        // accumulator rows per CTA
 constexpr int kBN = 256;                        // accumulator columns per tile, at most
@@ -51,7 +54,6 @@ constexpr int kAtomBytes = 64 * kBK * 2;        // MN-major: 64 rows of the oper
 constexpr int kThreads = 352;
 constexpr int kEpiWarps = 8;
 constexpr int kChunk = 32;                      // accumulator columns per epilogue step
-constexpr int kMinBn = 32;
 constexpr int kMaxSms = 256;                    // bound on the SM count used for planning
 constexpr int kHalf = 128;                      // accumulator columns of an epilogue thread
 constexpr int kSegBlocks = 16;                  // kLse: k blocks per accumulator in TMEM
@@ -60,25 +62,33 @@ constexpr int kNone = 0x7fffffff;               // sorted entry lists: no entry
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
+constexpr int kStageOut = 32 * 128;             // staging of an epilogue warp: 32 rows x 128 bytes
+
 template <int CG>
 struct Lay {
   static constexpr int kBBytes = kBN / CG * kBK * 2;          // this CTA's rows of B
   static constexpr int kStages = CG == 2 ? 6 : 4;
   static constexpr int oA = 0;
   static constexpr int oB = oA + kStages * kABytes;
-  static constexpr int oBar = oB + kStages * kBBytes;
+  static constexpr int oOut = oB + kStages * kBBytes;
+  static constexpr int oBar = oOut + kEpiWarps * kStageOut;
   static constexpr int oMisc = oBar + (2 * kStages + 4) * 8;
   static constexpr int kBytes = oMisc + 16 + 1024;            // + alignment slack
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
-constexpr bool a_mn_major(int mode) { return mode == kDw; }
-constexpr bool b_mn_major(int mode) { return mode == kDx || mode == kDw; }
+struct GemmMaps {
+  CUtensorMap a, b;           // operands; kGrad: of dx
+  CUtensorMap out;            // kDl: ds; kGrad: dx, as bf16 or as fp32 slots
+  CUtensorMap a2, b2, out2;   // kGrad: operands and result of dW
+};
 
 struct GemmArgs {
-  int R, N, K;                // rows of A, rows of B (columns of the result), contraction
-  int bn;                     // columns per tile (multiple of 16; kBN for an MN-major B)
+  int R, N;                   // rows of A, rows of B (columns of the result); kGrad: of dx
+  int bn;                     // columns per tile (kLse: multiple of 16, kDl: of 64, kGrad: kBN)
   int RT, NT, KB, KS, kbs, units;
+  int R2, RT2, KB2, units2;   // kGrad: the same of dW (columns as dx, no split)
+  int equal;                  // kGrad: tiles of dW that take the time of one of dx
   int32_t* status;
   int clear;                  // the call's first kernel: clear the status word
   int a_rows;                 // K-major A: rows per copy (fewer than kBM where R is)
@@ -93,11 +103,49 @@ struct GemmArgs {
   const float* lse;           // kDl
   const float* dloss;         // kDl
   float gscale;               // kDl: tau
-  __nv_bfloat16* out;         // kDl: ds; kDx (one slot), kDw: the result
-  int64_t ldo;
-  float* out32;               // kDx: fp32 slots [KS][R][N], or null
-  int filled;                 // kDx: slots that pieces before this one have written: add to them
+  int slots;                  // kGrad: dx goes to fp32 slots [KS][R][N]
+  int filled;                 // kGrad: slots that pieces before this one have written: add to them
 };
+
+// One tile: its rows of A (of the first CTA), rows of B, k blocks and split.
+struct Unit {
+  int row, col, k0, k1, ks;
+  bool w;                     // kGrad: a tile of dW
+};
+
+// The i-th tile of cluster c of n; false beyond the last.  Tiles go round-robin, row tile fastest,
+// so that the clusters of a round share the column operand and the row operand stays in L2.  In
+// kGrad the tiles of dx come first; the clusters that got one fewer take `equal` tiles of dW
+// before the others join in.
+template <int MODE, int CG>
+__device__ __forceinline__ bool unit_at(const GemmArgs& p, int c, int n, int i, Unit& u) {
+  int t = c + i * n;
+  if (MODE != kGrad || t < p.units) {
+    if (t >= p.units) return false;
+    const int rt = t % p.RT, rest = t / p.RT;
+    u.row = rt * CG * kBM;
+    u.col = rest % p.NT * p.bn;
+    u.ks = rest / p.NT;
+    u.k0 = u.ks * p.kbs;
+    u.k1 = min(p.KB, u.k0 + p.kbs);
+    u.w = false;
+    return true;
+  }
+  const int more = p.units % n;                   // clusters 0 .. more - 1 have one tile of dx more
+  const int j = i - (p.units / n + (c < more ? 1 : 0));
+  if (more == 0) t = j * n + c;
+  else if (c < more) t = p.equal * (n - more) + j * n + c;
+  else if (j < p.equal) t = j * (n - more) + c - more;
+  else t = p.equal * (n - more) + (j - p.equal) * n + c;
+  if (t >= p.units2) return false;
+  u.row = t % p.RT2 * CG * kBM;
+  u.col = t / p.RT2 * p.bn;
+  u.ks = 0;
+  u.k0 = 0;
+  u.k1 = p.KB2;
+  u.w = true;
+  return true;
+}
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -140,6 +188,45 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// TMA store of a staged box (2-D, or 3-D with the slot as the outermost coordinate), and its
+// adding form; completion is tracked by the issuing thread's bulk groups.
+__device__ __forceinline__ void tma_store_2d(const void* tmap, const void* src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(tmap)),
+               "r"(smem_u32(src)), "r"(x), "r"(y)
+               : "memory");
+}
+
+__device__ __forceinline__ void tma_store_3d(const void* tmap, const void* src, int x, int y, int z,
+                                             bool add) {
+  if (add)
+    asm volatile(
+        "cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, "
+        "%4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(tmap)),
+        "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+            reinterpret_cast<uint64_t>(tmap)),
+        "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+// The issuing thread's stores have read their shared memory.
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+
+// They are complete.
+__device__ __forceinline__ void bulk_wait() {
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
 // A token's ascending entry list, walked along with the columns of a tile.
 struct EntryWalk {
   const int32_t* e;
@@ -162,8 +249,7 @@ struct EntryWalk {
 
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1)
-    head_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
-                     const __grid_constant__ CUtensorMap tmB, const GemmArgs p) {
+    head_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
   using Lo = Lay<CG>;
   constexpr int kStages = Lo::kStages, kBBytes = Lo::kBBytes;
   extern __shared__ uint8_t smem_raw[];
@@ -180,11 +266,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int lane = threadIdx.x & 31;
   const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
   const int cid = static_cast<int>(blockIdx.x) / CG, ncl = static_cast<int>(gridDim.x) / CG;
-  // unit u = (split * NT + column tile) * RT + row tile: the CTAs of a wave share the column
-  // operand's tiles and the row operand stays in L2
-  auto unit_rt = [&](int u) { return u % p.RT; };
-  auto unit_nt = [&](int u) { return (u / p.RT) % p.NT; };
-  auto unit_ks = [&](int u) { return u / p.RT / p.NT; };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -197,8 +278,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     *abort_flag = 0;
     fence_barrier_init();
-    prefetch_tmap(&tmA);
-    prefetch_tmap(&tmB);
+    prefetch_tmap(&maps.a);
+    prefetch_tmap(&maps.b);
   }
   if (warp == 1) tmem_alloc_cg<CG>(tmem_slot, kTmemCols);
   tc_fence_before_sync();
@@ -208,35 +289,35 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
 
+  auto timed_out = [&]() {
+    report(p.status, FQ_ERR_TIMEOUT);
+    *abort_flag = 1;
+  };
+
   if (warp == 0 || warp == 10) {
     // ---------------------------------------------------------------- producers
     const bool is_a = warp == 0;
     pdl_wait();
     if (p.clear && blockIdx.x == 0 && is_a && lane == 0) *p.status = 0;
     __syncwarp();
-    // a B that is read once (one row tile) need not stay in L2
-    const uint64_t pol = !is_a && p.RT == 1 ? policy_evict_first() : policy_evict_last();
+    const uint64_t pol_keep = policy_evict_last(), pol_once = policy_evict_first();
     const int bn_cta = p.bn / CG;                   // rows of B of this CTA
-    const uint32_t bytes =
-        (a_mn_major(MODE) ? kABytes : static_cast<uint32_t>(p.a_rows) * kBK * 2) +
-        (b_mn_major(MODE) ? kBBytes : static_cast<uint32_t>(bn_cta) * kBK * 2);
-    const CUtensorMap* tm = is_a ? &tmA : &tmB;
-    const bool mn = is_a ? a_mn_major(MODE) : b_mn_major(MODE);
-    const int boxes = is_a ? kBM / 64 : kBN / CG / 64;           // of an MN-major operand
+    const uint32_t bytes = static_cast<uint32_t>(MODE == kGrad ? kABytes : p.a_rows * kBK * 2) +
+                           static_cast<uint32_t>(bn_cta) * kBK * 2;
     // the pair's copies count on the first CTA's barriers
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
-    auto load = [&](uint8_t* dst, int st, int x, int y) {
-      if (CG == 2) tma_load_2d_pair(dst, tm, full0 + static_cast<uint32_t>(st) * 8, x, y, pol);
-      else tma_load_2d(dst, tm, &full[st], x, y, pol);
-    };
     int stage = 0;
     uint32_t phase = 0;
     int64_t it = 0;
     bool ok = true;
-    for (int u = cid; ok && u < p.units; u += ncl) {
-      const int row = is_a ? (unit_rt(u) * CG + rank) * kBM : unit_nt(u) * p.bn + rank * bn_cta;
-      const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
-      for (int kb = k0; kb < k1; ++kb, ++it) {
+    Unit u;
+    for (int i = 0; ok && unit_at<MODE, CG>(p, cid, ncl, i, u); ++i) {
+      const CUtensorMap* tm = is_a ? (u.w ? &maps.a2 : &maps.a) : (u.w ? &maps.b2 : &maps.b);
+      const bool mn = MODE == kGrad && (!is_a || u.w);           // an MN-major operand
+      // W, where it is read once (one row tile), need not stay in L2
+      const uint64_t pol = !is_a && !u.w && p.RT == 1 ? pol_once : pol_keep;
+      const int row = is_a ? u.row + rank * kBM : u.col + rank * bn_cta;
+      for (int kb = u.k0; kb < u.k1; ++kb, ++it) {
         ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
         if (!ok) break;
         if (elect_one()) {
@@ -244,19 +325,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           // others' may arrive before that: the phase still waits for the one arrival.
           if (is_a && rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
           uint8_t* dst = smem + (is_a ? Lo::oA + stage * kABytes : Lo::oB + stage * kBBytes);
-          if (mn) {
-            for (int i = 0; i < boxes; ++i) load(dst + i * kAtomBytes, stage, row + 64 * i, kb * kBK);
-          } else {
-            load(dst, stage, kb * kBK, row);
+          const uint32_t bar = full0 + static_cast<uint32_t>(stage) * 8;
+#pragma unroll
+          for (int h = 0; h < (MODE == kGrad ? 2 : 1); ++h) {
+            const int x = mn ? row + 64 * h : kb * kBK, y = mn ? kb * kBK : row;
+            if (CG == 2) tma_load_2d_pair(dst + h * kAtomBytes, tm, bar, x, y, pol);
+            else tma_load_2d(dst + h * kAtomBytes, tm, &full[stage], x, y, pol);
+            if (!mn) break;
           }
         }
         if (++stage == kStages) stage = 0, phase ^= 1;
       }
     }
-    if (!ok) {
-      report(p.status, FQ_ERR_TIMEOUT);
-      *abort_flag = 1;
-    }
+    if (!ok) timed_out();
     // Never leave with copies in flight: a stage is released once the MMAs that read its copies
     // (of both CTAs) are done, so wait (bounded) for the release of every stage used.
     for (int s = 0; s < kStages; ++s) {
@@ -267,22 +348,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (rank == 0) {
-      const uint32_t idesc = umma_idesc_bf16(CG * kBM, static_cast<uint32_t>(p.bn)) |
-                             (a_mn_major(MODE) ? 1u << 15 : 0u) |
-                             (b_mn_major(MODE) ? 1u << 16 : 0u);
-      // 16 k per MMA: 32 bytes along a K-major row, or 16 rows of 128 bytes of an MN-major tile
-      constexpr uint64_t stepA = (a_mn_major(MODE) ? 2048 : 32) >> 4;
-      constexpr uint64_t stepB = (b_mn_major(MODE) ? 2048 : 32) >> 4;
       const uint32_t sa = smem_u32(smem + Lo::oA), sb = smem_u32(smem + Lo::oB);
-      const uint64_t ad0 = a_mn_major(MODE) ? umma_desc_mn(sa) : umma_desc_sw128(sa);
-      const uint64_t bd0 = b_mn_major(MODE) ? umma_desc_mn(sb) : umma_desc_sw128(sb);
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      for (int u = cid; ok && u < p.units; u += ncl) {
-        const int k0 = unit_ks(u) * p.kbs, k1 = min(p.KB, k0 + p.kbs);
-        for (int ka = k0; ok && ka < k1;) {
-          const int ke = MODE == kLse ? min(k1, ka + kSegBlocks) : k1;
+      Unit u;
+      for (int i = 0; ok && unit_at<MODE, CG>(p, cid, ncl, i, u); ++i) {
+        const bool amn = MODE == kGrad && u.w;
+        constexpr bool bmn = MODE == kGrad;
+        const uint32_t idesc = umma_idesc_bf16(CG * kBM, static_cast<uint32_t>(p.bn)) |
+                               (amn ? 1u << 15 : 0u) | (bmn ? 1u << 16 : 0u);
+        // 16 k per MMA: 32 bytes along a K-major row, or 16 rows of 128 bytes of an MN-major tile
+        const uint64_t stepA = (amn ? 2048 : 32) >> 4;
+        constexpr uint64_t stepB = (bmn ? 2048 : 32) >> 4;
+        const uint64_t ad0 = amn ? umma_desc_mn(sa) : umma_desc_sw128(sa);
+        const uint64_t bd0 = bmn ? umma_desc_mn(sb) : umma_desc_sw128(sb);
+        for (int ka = u.k0; ok && ka < u.k1;) {
+          const int ke = MODE == kLse ? min(u.k1, ka + kSegBlocks) : u.k1;
           ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
@@ -307,30 +389,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           ka = ke;
         }
       }
-      if (!ok) {
-        report(p.status, FQ_ERR_TIMEOUT);
-        *abort_flag = 1;
-      }
+      if (!ok) timed_out();
     }
   } else {
     // ---------------------------------------------------------------- epilogue
     const int quarter = warp & 3;                 // TMEM lanes 32 * quarter .. + 31
     const int half = (warp - 2) >> 2;
-    const int r_in_tile = quarter * 32 + lane;
-    // this thread's columns [h0, h1) of a tile
-    const int hw = (p.bn / 2 + kChunk - 1) / kChunk * kChunk;
-    const int h0 = half * hw, h1 = half ? p.bn : hw;
+    // this thread's columns [h0, h1) of a tile (kDl, kGrad: in whole steps of 64)
+    const int hw = (p.bn / 2 + 63) / 64 * 64;
+    const int h0 = half * hw, h1 = half ? p.bn : min(hw, p.bn);
+    uint8_t* out = smem + Lo::oOut + (warp - 2) * kStageOut;
     pdl_wait();
     int buf = 0;
     uint32_t acc_phase = 0;
     auto wait_acc = [&]() {
       // the warp leaves as one: the TMEM loads are warp-wide
-      if (__all_sync(0xffffffffu, mbar_wait(&tfull[buf], acc_phase, abort_flag))) {
+      if (mbar_wait_warp(&tfull[buf], acc_phase, abort_flag)) {
         tc_fence_after_sync();
         return true;
       }
-      report(p.status, FQ_ERR_TIMEOUT);
-      *abort_flag = 1;
+      timed_out();
       return false;
     };
     auto release_acc = [&]() {
@@ -342,15 +420,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (++buf == 2) buf = 0, acc_phase ^= 1;
     };
-    for (int u = cid; u < p.units; u += ncl) {
-      const int nt = unit_nt(u);
-      const int row = (unit_rt(u) * CG + rank) * kBM + r_in_tile;
-      const int n0 = nt * p.bn + h0;              // first column of this thread in the result
-      const bool row_ok = row < p.R;
-      const int64_t lrow = row_ok ? row : 0;
+    // Results leave through shared memory, 32 rows x 128 bytes at a time: this thread's row of a
+    // box as eight 16-byte chunks under the 128-byte swizzle, then one TMA store by the warp, which
+    // drops what lies beyond the result's rows and columns.
+    auto stage_begin = [&]() {
+      if (elect_one()) bulk_wait_read();
+      __syncwarp();
+    };
+    auto stage_chunk = [&](int c, uint32_t a, uint32_t b, uint32_t d, uint32_t e) {
+      *reinterpret_cast<uint4*>(out + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(a, b, d, e);
+    };
+    Unit u;
+    for (int i = 0; unit_at<MODE, CG>(p, cid, ncl, i, u); ++i) {
+      const int row_w = u.row + rank * kBM + quarter * 32;        // first row of the warp
+      const int row = row_w + lane;
+      const int n0 = u.col + h0;                  // first column of this thread in the result
       const int cols = min(h1 - h0, p.N - n0);    // valid columns of this thread (may be <= 0)
       const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + h0;
       if constexpr (MODE == kLse) {
+        const bool row_ok = row < p.R;
+        const int64_t lrow = row_ok ? row : 0;
         float acc[kHalf];
 #pragma unroll
         for (int q = 0; q < kHalf; ++q) acc[q] = 0.f;
@@ -397,91 +486,99 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int q = 0; q < 8; ++q) s += ex2(acc[c + q] - ref);
           sum += s;
         }
-        if (row_ok) p.part[(static_cast<int64_t>(nt) * 2 + half) * p.R + row] = make_float2(m, sum);
-      } else {
+        if (row_ok)
+          p.part[(static_cast<int64_t>(u.col / p.bn) * 2 + half) * p.R + row] = make_float2(m, sum);
+      } else if constexpr (MODE == kDl) {
+        const bool row_ok = row < p.R;
+        const int64_t lrow = row_ok ? row : 0;
+        EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, p.v0 + n0);
+        const float c2 = p.scale * kLog2e;
+        float lse2 = 0.f, g = 0.f;
+        bool has = false;
+        if (row_ok) {
+          const int first = __ldcg(p.entry + lrow * p.E);
+          has = first >= 0 && first < p.V;
+          lse2 = __ldcg(p.lse + row) * kLog2e;
+          g = __ldcg(p.dloss + row) * p.gscale;
+        }
         if (!wait_acc()) break;
         const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
-        if (MODE == kDl) {
-          EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, p.v0 + n0);
-          const float c2 = p.scale * kLog2e;
-          float lse2 = 0.f, g = 0.f;
-          bool has = false;
-          if (row_ok) {
-            const int first = __ldcg(p.entry + lrow * p.E);
-            has = first >= 0 && first < p.V;
-            lse2 = __ldcg(p.lse + row) * kLog2e;
-            g = __ldcg(p.dloss + row) * p.gscale;
-          }
+        const bool rows_any = row_w < p.R;
 #pragma unroll 1
-          for (int c = 0; c < cols; c += kChunk) {
+        for (int c = 0; rows_any && c < cols; c += 64) {
+          stage_begin();
+#pragma unroll
+          for (int cc = 0; cc < 64; cc += kChunk) {
             float v[kChunk];
             __syncwarp();
-            tmem_ld32(t_row + c, v);
+            tmem_ld32(t_row + c + cc, v);
             tmem_wait_ld();
 #pragma unroll
             for (int q = 0; q < kChunk; ++q) v[q] = ex2(fmaf(v[q], c2, -lse2));
-            while (w.next < p.v0 + n0 + c + kChunk) {
-              const int j = w.next - (p.v0 + n0 + c);
+            while (w.next < p.v0 + n0 + c + cc + kChunk) {
+              const int j = w.next - (p.v0 + n0 + c + cc);
               const float pk = p.prob ? __ldcg(p.prob + lrow * p.E + w.k) : 1.f;
 #pragma unroll
               for (int q = 0; q < kChunk; ++q) v[q] -= q == j ? pk : 0.f;
               w.step();
             }
-            if (row_ok) {
-              uint4* dst = reinterpret_cast<uint4*>(p.out + row * p.ldo + n0 + c);
 #pragma unroll
-              for (int q = 0; q < kChunk; q += 8) {
-                if (c + q >= h1 - h0) break;       // the next tile's columns
-                uint4 o;
-                o.x = has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u;
-                o.y = has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u;
-                o.z = has ? pack_bf16(g * v[q + 4], g * v[q + 5]) : 0u;
-                o.w = has ? pack_bf16(g * v[q + 6], g * v[q + 7]) : 0u;
-                dst[q / 8] = o;
-              }
-            }
+            for (int q = 0; q < kChunk; q += 8)
+              stage_chunk((cc + q) / 8, has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u,
+                          has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u,
+                          has ? pack_bf16(g * v[q + 4], g * v[q + 5]) : 0u,
+                          has ? pack_bf16(g * v[q + 6], g * v[q + 7]) : 0u);
           }
-        } else {
-          // result rows; N is a multiple of 8
-          const int ks = unit_ks(u);
-          float* o32 = p.out32 ? p.out32 + (static_cast<int64_t>(ks) * p.R + row) * p.N + n0
-                               : nullptr;
-          __nv_bfloat16* o16 = p.out + static_cast<int64_t>(row) * p.ldo + n0;
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (elect_one()) {
+            tma_store_2d(&maps.out, out, n0 + c, row_w);
+            bulk_commit();
+          }
+        }
+        release_acc();
+      } else {
+        if (!wait_acc()) break;
+        const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
+        const bool rows_any = row_w < (u.w ? p.R2 : p.R);
+        const bool wide = !u.w && p.slots;        // fp32, 32 columns a box; else bf16, 64
+        const int per = wide ? 32 : 64;
 #pragma unroll 1
-          for (int c = 0; c < cols; c += kChunk) {
-            float v[kChunk];
-            __syncwarp();
-            tmem_ld32(t_row + c, v);
+        for (int c = 0; rows_any && c < cols; c += per) {
+          stage_begin();
+          float v[32];
+          tmem_ld32(t_row + c, v);
+          tmem_wait_ld();
+          if (wide) {
+#pragma unroll
+            for (int q = 0; q < 32; q += 4)
+              stage_chunk(q / 4, __float_as_uint(v[q]), __float_as_uint(v[q + 1]),
+                          __float_as_uint(v[q + 2]), __float_as_uint(v[q + 3]));
+          } else {
+#pragma unroll
+            for (int q = 0; q < 32; q += 8)
+              stage_chunk(q / 8, pack_bf16(v[q], v[q + 1]), pack_bf16(v[q + 2], v[q + 3]),
+                          pack_bf16(v[q + 4], v[q + 5]), pack_bf16(v[q + 6], v[q + 7]));
+            tmem_ld32(t_row + c + 32, v);
             tmem_wait_ld();
-            if (!row_ok) continue;
 #pragma unroll
-            for (int q = 0; q < kChunk; q += 8) {
-              if (c + q >= cols) break;
-              if (MODE == kDx && o32) {
-#pragma unroll
-                for (int h = 0; h < 8; h += 4) {
-                  float4* dst = reinterpret_cast<float4*>(o32 + c + q + h);
-                  float4 o = make_float4(v[q + h], v[q + h + 1], v[q + h + 2], v[q + h + 3]);
-                  if (ks < p.filled) {
-                    const float4 old = *dst;
-                    o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
-                  }
-                  *dst = o;
-                }
-              } else {
-                uint4 o;
-                o.x = pack_bf16(v[q], v[q + 1]);
-                o.y = pack_bf16(v[q + 2], v[q + 3]);
-                o.z = pack_bf16(v[q + 4], v[q + 5]);
-                o.w = pack_bf16(v[q + 6], v[q + 7]);
-                *reinterpret_cast<uint4*>(o16 + c + q) = o;
-              }
-            }
+            for (int q = 0; q < 32; q += 8)
+              stage_chunk(4 + q / 8, pack_bf16(v[q], v[q + 1]), pack_bf16(v[q + 2], v[q + 3]),
+                          pack_bf16(v[q + 4], v[q + 5]), pack_bf16(v[q + 6], v[q + 7]));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (elect_one()) {
+            if (wide) tma_store_3d(&maps.out, out, n0 + c, row_w, u.ks, u.ks < p.filled);
+            else tma_store_2d(u.w ? &maps.out2 : &maps.out, out, n0 + c, row_w);
+            bulk_commit();
           }
         }
         release_acc();
       }
     }
+    __syncwarp();
+    if (MODE != kLse && elect_one()) bulk_wait();   // no store outlives its shared memory
   }
 
   // Every MMA has completed (each accumulator was waited for) and every stage was released
@@ -676,6 +773,22 @@ bool make_tmap(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// fp32 slots of rows x cols each, boxes of 32 columns x 32 rows of one slot
+bool make_slot_tmap(CUtensorMap* m, const void* base, int64_t slots, int64_t rows, int64_t cols) {
+  auto enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
+                        static_cast<cuuint64_t>(slots)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * 4,
+                           static_cast<cuuint64_t>(rows) * static_cast<cuuint64_t>(cols) * 4};
+  cuuint32_t box[3] = {32, 32, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides, box,
+             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int sm_count() {
@@ -741,12 +854,11 @@ fq_status prepare_gemm(int& clusters) {
 }
 
 template <int MODE, int CG>
-fq_status launch_gemm_cg(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g,
-                         cudaStream_t s) {
+fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, cudaStream_t s) {
   int clusters = 0;
   if (const fq_status st = prepare_gemm<MODE, CG>(clusters)) return st;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min(g.units, clusters) * CG));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min(g.units + g.units2, clusters) * CG));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Lay<CG>::kBytes;
   cfg.stream = s;
@@ -759,44 +871,27 @@ fq_status launch_gemm_cg(const CUtensorMap& a, const CUtensorMap& b, const GemmA
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, CG>, a, b, g) == cudaSuccess ? FQ_OK
-                                                                                      : FQ_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, CG>, m, g) == cudaSuccess ? FQ_OK
+                                                                                   : FQ_ERR_CUDA;
 }
 
-// CTAs per tile: a pair where the result has more than one CTA's rows.
+// CTAs per tile of the logit products: a pair where there are more than one CTA's tokens.
 int group_for(int R) { return R > kBM ? 2 : 1; }
 
 template <int MODE>
-fq_status launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmArgs& g,
-                      cudaStream_t s) {
-  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(a, b, g, s)
-                             : launch_gemm_cg<MODE, 1>(a, b, g, s);
+fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, cudaStream_t s) {
+  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(m, g, s) : launch_gemm_cg<MODE, 1>(m, g, s);
 }
 
-void plan(GemmArgs& g, int R, int N, int K, int bn, int splits) {
-  g.R = R;
-  g.N = N;
-  g.K = K;
-  g.bn = bn;
-  // rows of the accumulator beyond R are never read, so what A's stage holds there (earlier
-  // copies, or nothing yet) does not matter
-  g.a_rows = static_cast<int>(std::min<int64_t>(kBM, round_up(R, 8)));
-  g.RT = static_cast<int>(ceil_div(R, kBM * group_for(R)));
-  g.NT = static_cast<int>(ceil_div(N, bn));
-  g.KB = static_cast<int>(ceil_div(K, kBK));
-  g.kbs = static_cast<int>(ceil_div(g.KB, splits));
-  g.KS = static_cast<int>(ceil_div(g.KB, g.kbs));
-  g.units = g.RT * g.NT * g.KS;
-}
-
-// Columns per tile of the logit products.  A tile's time hardly depends on its width (19.4 us at
-// 128 columns and 23.0 us at 256 for d = 4096, CG = 2), so tiles are as wide as they go, unless
-// all of them fit the SMs (or pairs) at once: then they are as narrow as still does.
-int pick_bn(int R, int N, int sms) {
+// Columns per tile of the logit products, a multiple of `unit`.  A tile's time hardly depends on
+// its width (19.4 us at 128 columns and 23.0 us at 256 for d = 4096, CG = 2), so tiles are as wide
+// as they go, unless all of them fit the SMs (or pairs) at once: then they are as narrow as still
+// does.
+int pick_bn(int R, int N, int sms, int unit) {
   const int cg = group_for(R);
   const int64_t RT = ceil_div(R, kBM * cg), room = std::min(sms, kMaxSms) / cg;
   int bn = kBN;
-  while (bn > kMinBn && RT * ceil_div(N, bn - 16 * cg) <= room) bn -= 16 * cg;
+  while (bn > unit && RT * ceil_div(N, bn - unit) <= room) bn -= unit;
   return bn;
 }
 
@@ -804,6 +899,24 @@ int pick_bn(int R, int N, int sms) {
 int64_t most_tiles(int R, int N) {
   const int cg = group_for(R);
   return std::max<int64_t>(ceil_div(N, kBN), kMaxSms / cg / ceil_div(R, kBM * cg));
+}
+
+// The tiles and operand maps of a logit product: R tokens x N vocabulary entries.
+bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, int N, int d,
+                 int sms, int unit) {
+  const int cg = group_for(R);
+  g.R = R;
+  g.N = N;
+  g.bn = pick_bn(R, N, sms, unit);
+  g.RT = static_cast<int>(ceil_div(R, kBM * cg));
+  g.NT = static_cast<int>(ceil_div(N, g.bn));
+  g.KB = g.kbs = static_cast<int>(ceil_div(d, kBK));
+  g.KS = 1;
+  g.units = g.RT * g.NT;
+  // rows of the accumulator beyond R are never read, so what A's stage holds there (earlier
+  // copies, or nothing yet) does not matter
+  g.a_rows = static_cast<int>(std::min<int64_t>(kBM, round_up(R, 8)));
+  return make_tmap(&m.a, x, R, d, d, g.a_rows) && make_tmap(&m.b, W, N, d, d, g.bn / cg);
 }
 
 constexpr int64_t kPieceBytes = 128ll << 20;    // ds of one piece of the vocabulary
@@ -818,12 +931,12 @@ int piece_width(int M, int V) {
   return static_cast<int>(std::min<int64_t>(round_up(V, 256), round_up(ceil_div(V, n), 256)));
 }
 
-// Ways the contraction of dx over a piece is split, so that few tiles still fill the SMs.
-int dx_splits(int M, int d, int Vc, int sms) {
-  const int64_t tiles = ceil_div(M, kBM * group_for(M)) * group_for(M) * ceil_div(d, kBN);
-  const int64_t KB = ceil_div(Vc, kBK);
+// Most ways the contraction of dx over a piece is split, so that few tiles still fill the SMs.
+int most_splits(int M, int d, int Vc, int sms) {
+  const int64_t tiles = ceil_div(M, 2 * kBM) * ceil_div(d, kBN);
   return static_cast<int>(std::max<int64_t>(
-      1, std::min<int64_t>({kMaxSlots, std::min(sms, kMaxSms) / tiles, KB / 8})));
+      1, std::min<int64_t>({kMaxSlots, std::min(sms, kMaxSms) / 2 / tiles,
+                            ceil_div(Vc, kBK) / 8})));
 }
 
 struct Ws {
@@ -851,7 +964,7 @@ Ws ws_layout(int M, int d, int V, int K, bool grad) {
     // the pitch leaves room for the last tile's columns beyond the piece
     L.ds = take(static_cast<size_t>(M) * (P + kBN) * 2);
     // sized for any SM count
-    const int S = dx_splits(M, d, std::min(P, V), kMaxSms);
+    const int S = most_splits(M, d, std::min(P, V), kMaxSms);
     L.slots = take(S > 1 || P < V ? static_cast<size_t>(S) * M * d * 4 : 0);
   }
   L.total = off;
@@ -922,10 +1035,8 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   char* ws = static_cast<char*>(wsv);
   const int sms = sm_count();
   GemmArgs g{};
-  plan(g, M, V, d, pick_bn(M, V, sms), 1);
-  CUtensorMap mx, mw;
-  if (!make_tmap(&mx, x, M, d, d, g.a_rows) || !make_tmap(&mw, W, V, d, d, g.bn / group_for(M)))
-    return FQ_ERR_CUDA;
+  GemmMaps m{};
+  if (!plan_logits(g, m, x, W, M, V, d, sms, 16 * group_for(M))) return FQ_ERR_CUDA;
   const float* plogp = nullptr;
   if (const fq_status st = launch_entries(t, M, V, L, ws, g.entry, g.prob, plogp, s)) return st;
   g.status = reinterpret_cast<int32_t*>(ws);
@@ -935,7 +1046,7 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   g.V = V;
   g.part = reinterpret_cast<float2*>(ws + L.part);
   g.zt = reinterpret_cast<float*>(ws + L.zt);
-  if (const fq_status st = launch_gemm<kLse>(mx, mw, g, s)) return st;
+  if (const fq_status st = launch_logits<kLse>(m, g, s)) return st;
   return launch(head_join_kernel, ceil_div(M, kJoinWarps), 32 * kJoinWarps, 0, s,
                 static_cast<const float2*>(g.part), 2 * g.NT, M, V, t.given, g.entry, g.prob,
                 static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, loss,
@@ -973,17 +1084,21 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
   const int P = piece_width(M, V);
   const int pieces = static_cast<int>(ceil_div(V, P));
   const int64_t ldds = P + kBN;
-  const int splits = dx_splits(M, d, std::min(P, V), sms);
-  const bool direct = splits == 1 && pieces == 1;
+  const int most = most_splits(M, d, std::min(P, V), sms);
+  // tiles of dx and of dW, in k blocks
+  const int RT = static_cast<int>(ceil_div(M, 2 * kBM)), NT = static_cast<int>(ceil_div(d, kBN));
+  const int KBm = static_cast<int>(ceil_div(M, kBK));
+  constexpr int kTile = 6;            // what a tile of dW takes besides its k blocks
   int used = 0;
+  bool direct = false;
   for (int q = 0; q < pieces; ++q) {
     const int v0 = q * P, Vc = std::min(P, V - v0);
     const __nv_bfloat16* Wq = Wb + static_cast<int64_t>(v0) * d;
-    CUtensorMap mx, mw;
     {
       GemmArgs g{};
-      plan(g, M, Vc, d, pick_bn(M, Vc, sms), 1);
-      if (!make_tmap(&mx, xc, M, d, d, g.a_rows) || !make_tmap(&mw, Wq, Vc, d, d, g.bn / group_for(M)))
+      GemmMaps m{};
+      if (!plan_logits(g, m, xc, Wq, M, Vc, d, sms, 64) ||
+          !make_tmap(&m.out, ds, M, Vc, ldds, 32))
         return FQ_ERR_CUDA;
       g.status = status;
       g.scale = 1.f / t.tau;
@@ -995,34 +1110,49 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.lse = lse;
       g.dloss = dloss;
       g.gscale = t.logit ? t.tau : 1.f;
-      g.out = ds;
-      g.ldo = ldds;
-      if (const fq_status st = launch_gemm<kDl>(mx, mw, g, s)) return st;
+      if (const fq_status st = launch_logits<kDl>(m, g, s)) return st;
     }
-    CUtensorMap ma, mb;
+    GemmArgs g{};
+    GemmMaps m{};
+    g.R = M;
+    g.N = d;
+    g.bn = kBN;
+    g.RT = RT;
+    g.NT = NT;
+    g.KB = static_cast<int>(ceil_div(Vc, kBK));
+    g.status = status;
+    const int RT2 = static_cast<int>(ceil_div(Vc, 2 * kBM));
     if (dx) {
-      GemmArgs g{};
-      plan(g, M, d, Vc, kBN, splits);
-      if (!make_tmap(&ma, ds, M, Vc, ldds, g.a_rows) || !make_tmap(&mb, Wq, Vc, d, d, kBK))
-        return FQ_ERR_CUDA;
-      g.status = status;
-      g.out = static_cast<__nv_bfloat16*>(dx);
-      g.ldo = d;
-      g.out32 = direct ? nullptr : slots;
+      // no split of dx longer than half of a pair's share of the work, if there are few tiles
+      const int64_t work = static_cast<int64_t>(RT) * NT * g.KB +
+                           (dW ? static_cast<int64_t>(RT2) * NT * (KBm + kTile) : 0);
+      const int64_t share = std::max<int64_t>(1, work / (sms / 2));
+      const int splits = static_cast<int>(
+          std::min<int64_t>(most, std::max<int64_t>(1, ceil_div(2 * g.KB, share))));
+      g.kbs = static_cast<int>(ceil_div(g.KB, splits));
+      g.KS = static_cast<int>(ceil_div(g.KB, g.kbs));
+      g.units = RT * NT * g.KS;
+      direct = pieces == 1 && g.KS == 1;
+      g.slots = !direct;
       g.filled = used;
       used = std::max(used, g.KS);
-      if (const fq_status st = launch_gemm<kDx>(ma, mb, g, s)) return st;
+      if (!make_tmap(&m.a, ds, M, Vc, ldds, kBM) || !make_tmap(&m.b, Wq, Vc, d, d, kBK) ||
+          !(direct ? make_tmap(&m.out, dx, M, d, d, 32)
+                   : make_slot_tmap(&m.out, slots, used, M, d)))
+        return FQ_ERR_CUDA;
     }
     if (dW) {
-      GemmArgs g{};
-      plan(g, Vc, d, M, kBN, 1);
-      if (!make_tmap(&ma, ds, M, Vc, ldds, kBK) || !make_tmap(&mb, xc, M, d, d, kBK))
+      g.R2 = Vc;
+      g.RT2 = RT2;
+      g.KB2 = KBm;
+      g.units2 = RT2 * NT;
+      g.equal = static_cast<int>(std::max<int64_t>(1, (g.kbs + (KBm + kTile) / 2) / (KBm + kTile)));
+      if (!make_tmap(&m.a2, ds, M, Vc, ldds, kBK) || !make_tmap(&m.b2, xc, M, d, d, kBK) ||
+          !make_tmap(&m.out2, static_cast<__nv_bfloat16*>(dW) + static_cast<int64_t>(v0) * d, Vc, d,
+                     d, 32))
         return FQ_ERR_CUDA;
-      g.status = status;
-      g.out = static_cast<__nv_bfloat16*>(dW) + static_cast<int64_t>(v0) * d;
-      g.ldo = d;
-      if (const fq_status st = launch_gemm<kDw>(ma, mb, g, s)) return st;
     }
+    if (const fq_status st = launch_gemm_cg<kGrad, 2>(m, g, s)) return st;
   }
   if (dx && !direct) {
     const int64_t n4 = static_cast<int64_t>(M) * d / 4;
