@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "fq_internal.h"
 
@@ -46,6 +47,26 @@ fq_status check_packed(const fq_packed* C) {
   if (C->bits != 2) return FQ_ERR_UNSUPPORTED;
   if (!aligned16(C->words) || !aligned16(C->scale_f16) || !aligned16(C->zero_f16))
     return FQ_ERR_ALIGNMENT;
+  return FQ_OK;
+}
+
+fq_status device_sms(int& sms) {
+  constexpr int kDevices = 64;
+  static std::atomic<int> known[kDevices];      // SMs, or -1 where the device is another one
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
+  int n = dev < kDevices ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    int major = 0, minor = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+      return FQ_ERR_CUDA;
+    if (major * 10 + minor != 103) n = -1;
+    if (dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
+  }
+  if (n < 0) return FQ_ERR_UNSUPPORTED;
+  sms = n;
   return FQ_OK;
 }
 

@@ -63,19 +63,14 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 constexpr int kStageOut = 32 * 128;             // staging of an epilogue warp: 32 rows x 128 bytes
+constexpr int kMaxStages = 12;
+constexpr int kTailBytes = (2 * kMaxStages + 4) * 8 + 16;     // barriers, TMEM address, abort flag
+constexpr int kSmemMost = 227 * 1024;
+constexpr int kRoom = 10 * 1024;                // left for blocks of the next kernel to wait in
 
-template <int CG>
-struct Lay {
-  static constexpr int kBBytes = kBN / CG * kBK * 2;          // this CTA's rows of B
-  static constexpr int kStages = CG == 2 ? 6 : 4;
-  static constexpr int oA = 0;
-  static constexpr int oB = oA + kStages * kABytes;
-  static constexpr int oOut = oB + kStages * kBBytes;
-  static constexpr int oBar = oOut + kEpiWarps * kStageOut;
-  static constexpr int oMisc = oBar + (2 * kStages + 4) * 8;
-  static constexpr int kBytes = oMisc + 16 + 1024;            // + alignment slack
-  static_assert(kBytes <= 227 * 1024, "shared memory");
-};
+// Shared memory: p.stages x (this CTA's rows of A, of B), the staging of results (not kLse), the
+// tail; 1 KiB of alignment slack.
+constexpr int out_bytes(int mode) { return mode == kLse ? 0 : kEpiWarps * kStageOut; }
 
 struct GemmMaps {
   CUtensorMap a, b;           // operands; kGrad: of dx
@@ -92,6 +87,8 @@ struct GemmArgs {
   int32_t* status;
   int clear;                  // the call's first kernel: clear the status word
   int a_rows;                 // K-major A: rows per copy (fewer than kBM where R is)
+  int stages, stage_bytes, b_off;               // ring of operand stages; B's place in one
+  int early_a, early_b;       // the operand (of dx) does not depend on the kernel before this one
   // kLse, kDl
   float scale;                // 1 / tau
   const int32_t* entry;       // [R][E] vocabulary entries of each token's target, ascending
@@ -250,16 +247,15 @@ struct EntryWalk {
 template <int MODE, int CG>
 __global__ void __launch_bounds__(kThreads, 1)
     head_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmArgs p) {
-  using Lo = Lay<CG>;
-  constexpr int kStages = Lo::kStages, kBBytes = Lo::kBBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + Lo::oBar);   // used in the pair's first CTA
-  uint64_t* empty = full + kStages;
-  uint64_t* tfull = empty + kStages;
+  uint8_t* staging = smem + p.stages * p.stage_bytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + out_bytes(MODE));   // first CTA's
+  uint64_t* empty = full + kMaxStages;
+  uint64_t* tfull = empty + kMaxStages;
   uint64_t* tempty = tfull + 2;                                    // used in the pair's first CTA
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + Lo::oMisc);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tempty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
@@ -268,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int cid = static_cast<int>(blockIdx.x) / CG, ncl = static_cast<int>(gridDim.x) / CG;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < p.stages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -297,12 +293,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0 || warp == 10) {
     // ---------------------------------------------------------------- producers
     const bool is_a = warp == 0;
-    pdl_wait();
+    // an operand that a user gave needs no wait once an earlier kernel of the call has done it
+    bool waited = !(is_a ? p.early_a : p.early_b);
+    if (waited) pdl_wait();
     if (p.clear && blockIdx.x == 0 && is_a && lane == 0) *p.status = 0;
     __syncwarp();
     const uint64_t pol_keep = policy_evict_last(), pol_once = policy_evict_first();
     const int bn_cta = p.bn / CG;                   // rows of B of this CTA
-    const uint32_t bytes = static_cast<uint32_t>(MODE == kGrad ? kABytes : p.a_rows * kBK * 2) +
+    const uint32_t bytes = static_cast<uint32_t>(p.a_rows * kBK * 2) +
                            static_cast<uint32_t>(bn_cta) * kBK * 2;
     // the pair's copies count on the first CTA's barriers
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
@@ -317,6 +315,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       // W, where it is read once (one row tile), need not stay in L2
       const uint64_t pol = !is_a && !u.w && p.RT == 1 ? pol_once : pol_keep;
       const int row = is_a ? u.row + rank * kBM : u.col + rank * bn_cta;
+      if (!waited && u.w) {
+        pdl_wait();
+        waited = true;
+      }
       for (int kb = u.k0; kb < u.k1; ++kb, ++it) {
         ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
         if (!ok) break;
@@ -324,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // A's producer of the first CTA expects the bytes of both producers and CTAs.  The
           // others' may arrive before that: the phase still waits for the one arrival.
           if (is_a && rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
-          uint8_t* dst = smem + (is_a ? Lo::oA + stage * kABytes : Lo::oB + stage * kBBytes);
+          uint8_t* dst = smem + stage * p.stage_bytes + (is_a ? 0 : p.b_off);
           const uint32_t bar = full0 + static_cast<uint32_t>(stage) * 8;
 #pragma unroll
           for (int h = 0; h < (MODE == kGrad ? 2 : 1); ++h) {
@@ -334,21 +336,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!mn) break;
           }
         }
-        if (++stage == kStages) stage = 0, phase ^= 1;
+        if (++stage == p.stages) stage = 0, phase ^= 1;
       }
     }
     if (!ok) timed_out();
     // Never leave with copies in flight: a stage is released once the MMAs that read its copies
     // (of both CTAs) are done, so wait (bounded) for the release of every stage used.
-    for (int s = 0; s < kStages; ++s) {
-      const int64_t uses = it / kStages + (s < it % kStages ? 1 : 0);
+    for (int s = 0; s < p.stages; ++s) {
+      const int64_t uses = it / p.stages + (s < it % p.stages ? 1 : 0);
       if (uses > 0 && !mbar_wait(&empty[s], static_cast<uint32_t>(uses - 1) & 1u, nullptr))
         report(p.status, FQ_ERR_TIMEOUT);
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (rank == 0) {
-      const uint32_t sa = smem_u32(smem + Lo::oA), sb = smem_u32(smem + Lo::oB);
+      const uint32_t sa = smem_u32(smem), sb = sa + static_cast<uint32_t>(p.b_off);
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
@@ -372,8 +374,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int kb = ka; kb < ke; ++kb) {
             ok = mbar_wait_warp(&full[stage], phase, abort_flag);
             if (!ok) break;
-            const uint64_t ad = ad0 + static_cast<uint32_t>(stage * (kABytes >> 4));
-            const uint64_t bd = bd0 + static_cast<uint32_t>(stage * (kBBytes >> 4));
+            const uint32_t at = static_cast<uint32_t>(stage * p.stage_bytes) >> 4;
+            const uint64_t ad = ad0 + at, bd = bd0 + at;
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < kBK / 16; ++k)
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             (kb > ka || k > 0) ? 1u : 0u);
               umma_commit_cg<CG>(&empty[stage]);
             }
-            if (++stage == kStages) stage = 0, phase ^= 1;
+            if (++stage == p.stages) stage = 0, phase ^= 1;
           }
           if (!ok) break;
           if (elect_one()) umma_commit_cg<CG>(&tfull[buf]);
@@ -398,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // this thread's columns [h0, h1) of a tile (kDl, kGrad: in whole steps of 64)
     const int hw = (p.bn / 2 + 63) / 64 * 64;
     const int h0 = half * hw, h1 = half ? p.bn : min(hw, p.bn);
-    uint8_t* out = smem + Lo::oOut + (warp - 2) * kStageOut;
+    uint8_t* out = staging + (warp - 2) * kStageOut;
     pdl_wait();
     int buf = 0;
     uint32_t acc_phase = 0;
@@ -621,8 +623,9 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   __shared__ int32_t idx[FQ_DISTILL_MAX_K];
   __shared__ float tl[FQ_DISTILL_MAX_K];
   __shared__ float red[kSortThreads / 32];
-  pdl_launch_dependents();
+  // what follows may read the user's inputs at once: all that came before this call is complete
   pdl_wait();
+  pdl_launch_dependents();
   const int64_t base = static_cast<int64_t>(blockIdx.x) * K;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
@@ -665,43 +668,70 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   if (threadIdx.x == 0) plogp[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// One warp per token: joins the tiles' maxima and sums, then the loss.  Reports targets beyond
-// the vocabulary.
-constexpr int kJoinWarps = 4;
+// Joins the tiles' maxima and sums of each token, then the loss; reports targets beyond the
+// vocabulary.  A block takes `rows` tokens (1 or 8): neighbouring
+// lanes are neighbouring tokens, and the 256 / rows threads of a token share its tiles and its
+// entries.  Parts are joined in a fixed order.
+constexpr int kJoinThreads = 256;
 
-__global__ void __launch_bounds__(32 * kJoinWarps) head_join_kernel(
+__global__ void __launch_bounds__(kJoinThreads) head_join_kernel(
     const float2* part, int NT, int M, int V, const int32_t* given, const int32_t* entry,
-    const float* prob, const float* zt, const float* plogp, int E, float tau2, float* loss,
-    float* lse, int32_t* status) {
+    const float* prob, const float* zt, const float* plogp, int E, float tau2, int rows,
+    float* loss, float* lse, int32_t* status) {
+  constexpr int kWarps = kJoinThreads / 32;
+  __shared__ float2 red[kWarps][8];
+  __shared__ float sum[kWarps][8];
   pdl_launch_dependents();
   pdl_wait();
-  const int row = blockIdx.x * kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (row >= M) return;
-  const int64_t base = static_cast<int64_t>(row) * E;
-  bool bad = false;
-  for (int k = lane; k < E; k += 32) bad |= __ldcg(given + base + k) >= V;
-  if (__any_sync(0xffffffffu, bad) && lane == 0) report(status, FQ_ERR_DEVICE_CHECK);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = lane & (rows - 1);
+  const int g = rows == 1 ? static_cast<int>(threadIdx.x) : static_cast<int>(threadIdx.x) >> 3;
+  const int groups = rows == 1 ? kJoinThreads : kJoinThreads / 8;
+  const int row = blockIdx.x * rows + r;
+  const bool ok = row < M;
+  const int64_t base = static_cast<int64_t>(ok ? row : 0) * E;
   float m = -CUDART_INF_F, s = 0.f;
-  for (int t = lane; t < NT; t += 32) {
-    const float2 q = __ldcg(part + static_cast<int64_t>(t) * M + row);
+  auto join = [&](float2 q) {
     const float mn = fmaxf(m, q.x);
     const float ref = mn == -CUDART_INF_F ? 0.f : mn;
     s = s * exp2f(m - ref) + q.y * exp2f(q.x - ref);
     m = mn;
+  };
+  if (ok) {
+#pragma unroll 4
+    for (int t = g; t < NT; t += groups) join(__ldcg(part + static_cast<int64_t>(t) * M + row));
   }
-  const float top = warp_max(m);
-  const float ref = top == -CUDART_INF_F ? 0.f : top;
-  s = warp_sum(s * exp2f(m - ref));
-  const float l = (ref + log2f(s)) * kLn2;
+  for (int o = 16; o >= rows; o >>= 1) {
+    const float2 q = make_float2(__shfl_xor_sync(0xffffffffu, m, o),
+                                 __shfl_xor_sync(0xffffffffu, s, o));
+    join(q);
+  }
+  if (lane < rows) red[warp][r] = make_float2(m, s);
+  __syncthreads();
+  m = -CUDART_INF_F;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) join(red[w][r]);
+  const float l = ((m == -CUDART_INF_F ? 0.f : m) + log2f(s)) * kLn2;
   float d = 0.f;
-  for (int k = lane; k < E; k += 32) {
-    const int32_t i = __ldcg(entry + base + k);
-    if (i < 0 || i >= V) continue;
-    const float pk = prob ? __ldcg(prob + base + k) : 1.f;
-    d += pk == 0.f ? 0.f : pk * (l - __ldcg(zt + base + k));
+  bool bad = false;
+  if (ok) {
+    for (int k = g; k < E; k += groups) {
+      bad |= __ldcg(given + base + k) >= V;
+      const int32_t i = __ldcg(entry + base + k);
+      if (i < 0 || i >= V) continue;
+      const float pk = prob ? __ldcg(prob + base + k) : 1.f;
+      d += pk == 0.f ? 0.f : pk * (l - __ldcg(zt + base + k));
+    }
   }
-  d = warp_sum(d);
-  if (lane == 0) {
+  if (bad) report(status, FQ_ERR_DEVICE_CHECK);
+  for (int o = 16; o >= rows; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if (lane < rows) sum[warp][r] = d;
+  __syncthreads();
+  if (ok && static_cast<int>(threadIdx.x) < rows) {
+    d = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) d += sum[w][r];
     const int32_t first = __ldcg(entry + base);
     const bool has = first >= 0 && first < V;
     loss[row] = has ? tau2 * (d + (plogp ? __ldcg(plogp + row) : 0.f)) : 0.f;
@@ -715,8 +745,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) head_join_kernel(
 __global__ void __launch_bounds__(256) head_mask_rows_kernel(const uint4* x, int d8,
                                                              const int32_t* entry, int E, int V,
                                                              uint4* xc, int32_t* status) {
-  pdl_launch_dependents();
   pdl_wait();
+  pdl_launch_dependents();                        // as in head_entries_kernel
   if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   const int64_t row = blockIdx.x;
   const int32_t first = __ldcg(entry + row * E);
@@ -791,13 +821,6 @@ bool make_slot_tmap(CUtensorMap* m, const void* base, int64_t slots, int64_t row
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-int sm_count() {
-  int dev = 0, n = 0;
-  cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-  return n > 0 ? n : 148;
-}
-
 template <typename... Params, typename... Args>
 cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem,
                    cudaStream_t s, Args... args) {
@@ -816,7 +839,7 @@ cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t sm
 
 // CTA pairs that fit the device at once (its SMs in pairs, where the launch limits allow).
 template <int MODE, int CG>
-fq_status prepare_gemm(int& clusters) {
+fq_status prepare_gemm(int sms, int& clusters) {
   static std::mutex mu;
   static std::map<int, int> fit;
   int dev = 0;
@@ -826,14 +849,14 @@ fq_status prepare_gemm(int& clusters) {
   if (it == fit.end()) {
     if (cudaFuncSetAttribute(head_gemm_kernel<MODE, CG>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             Lay<CG>::kBytes) != cudaSuccess)
+                             kSmemMost) != cudaSuccess)
       return FQ_ERR_CUDA;
-    int n = sm_count();
+    int n = sms;
     if (CG == 2) {
       cudaLaunchConfig_t cfg{};
       cfg.gridDim = dim3(static_cast<unsigned>(n / 2 * 2));
       cfg.blockDim = dim3(kThreads);
-      cfg.dynamicSmemBytes = Lay<CG>::kBytes;
+      cfg.dynamicSmemBytes = kSmemMost;
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = 2;
@@ -854,13 +877,16 @@ fq_status prepare_gemm(int& clusters) {
 }
 
 template <int MODE, int CG>
-fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, cudaStream_t s) {
+fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, int sms, cudaStream_t s) {
   int clusters = 0;
-  if (const fq_status st = prepare_gemm<MODE, CG>(clusters)) return st;
+  if (const fq_status st = prepare_gemm<MODE, CG>(sms, clusters)) return st;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(std::min(g.units + g.units2, clusters) * CG));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Lay<CG>::kBytes;
+  // the MMA reads kBM rows of A, of which a stage may hold fewer: the last stage's too lie inside
+  const int last = (g.stages - 1) * g.stage_bytes + kABytes;
+  cfg.dynamicSmemBytes = static_cast<size_t>(
+      1024 + std::max(last, g.stages * g.stage_bytes + out_bytes(MODE) + kTailBytes));
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -879,8 +905,9 @@ fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, cudaStream_t s) {
 int group_for(int R) { return R > kBM ? 2 : 1; }
 
 template <int MODE>
-fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, cudaStream_t s) {
-  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(m, g, s) : launch_gemm_cg<MODE, 1>(m, g, s);
+fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStream_t s) {
+  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(m, g, sms, s)
+                             : launch_gemm_cg<MODE, 1>(m, g, sms, s);
 }
 
 // Columns per tile of the logit products, a multiple of `unit`.  A tile's time hardly depends on
@@ -901,13 +928,21 @@ int64_t most_tiles(int R, int N) {
   return std::max<int64_t>(ceil_div(N, kBN), kMaxSms / cg / ceil_div(R, kBM * cg));
 }
 
+void plan_ring(GemmArgs& g, int mode, int a_bytes, int b_bytes) {
+  g.b_off = a_bytes;
+  g.stage_bytes = a_bytes + b_bytes;
+  g.stages = std::min(kMaxStages,
+                      (kSmemMost - (mode == kLse ? kRoom : 0) - 1024 - kTailBytes - out_bytes(mode)) /
+                          g.stage_bytes);
+}
+
 // The tiles and operand maps of a logit product: R tokens x N vocabulary entries.
 bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, int N, int d,
-                 int sms, int unit) {
+                 int sms, int mode) {
   const int cg = group_for(R);
   g.R = R;
   g.N = N;
-  g.bn = pick_bn(R, N, sms, unit);
+  g.bn = pick_bn(R, N, sms, mode == kDl ? 64 : 16 * cg);
   g.RT = static_cast<int>(ceil_div(R, kBM * cg));
   g.NT = static_cast<int>(ceil_div(N, g.bn));
   g.KB = g.kbs = static_cast<int>(ceil_div(d, kBK));
@@ -916,6 +951,7 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
   // rows of the accumulator beyond R are never read, so what A's stage holds there (earlier
   // copies, or nothing yet) does not matter
   g.a_rows = static_cast<int>(std::min<int64_t>(kBM, round_up(R, 8)));
+  plan_ring(g, mode, static_cast<int>(round_up(g.a_rows * kBK * 2, 1024)), g.bn / cg * kBK * 2);
   return make_tmap(&m.a, x, R, d, d, g.a_rows) && make_tmap(&m.b, W, N, d, d, g.bn / cg);
 }
 
@@ -931,12 +967,12 @@ int piece_width(int M, int V) {
   return static_cast<int>(std::min<int64_t>(round_up(V, 256), round_up(ceil_div(V, n), 256)));
 }
 
-// Most ways the contraction of dx over a piece is split, so that few tiles still fill the SMs.
+// Most ways the contraction of dx over a piece is split: where its tiles are fewer than the pairs.
 int most_splits(int M, int d, int Vc, int sms) {
   const int64_t tiles = ceil_div(M, 2 * kBM) * ceil_div(d, kBN);
+  if (tiles >= std::min(sms, kMaxSms) / 2) return 1;
   return static_cast<int>(std::max<int64_t>(
-      1, std::min<int64_t>({kMaxSlots, std::min(sms, kMaxSms) / 2 / tiles,
-                            ceil_div(Vc, kBK) / 8})));
+      1, std::min<int64_t>(kMaxSlots, ceil_div(Vc, kBK) / 8)));
 }
 
 struct Ws {
@@ -993,15 +1029,6 @@ fq_status check_common(const void* x, int M, int d, const void* W, int V, const 
   return FQ_OK;
 }
 
-fq_status check_device() {
-  int dev = 0, major = 0, minor = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-    return FQ_ERR_CUDA;
-  return major * 10 + minor == 103 ? FQ_OK : FQ_ERR_UNSUPPORTED;
-}
-
 // The token's entries in ascending order: the target itself, or the sorted teacher's list.
 fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws,
                          const int32_t*& entry, const float*& prob, const float*& plogp,
@@ -1030,27 +1057,31 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
     return st;
   if (!loss) return FQ_ERR_INVALID_ARG;
   if (!aligned16(loss)) return FQ_ERR_ALIGNMENT;
-  if (const fq_status st = check_device()) return st;
+  int sms = 0;
+  if (const fq_status st = device_sms(sms)) return st;
   const Ws L = ws_layout(M, d, V, t.K, false);
   char* ws = static_cast<char*>(wsv);
-  const int sms = sm_count();
   GemmArgs g{};
   GemmMaps m{};
-  if (!plan_logits(g, m, x, W, M, V, d, sms, 16 * group_for(M))) return FQ_ERR_CUDA;
+  if (!plan_logits(g, m, x, W, M, V, d, sms, kLse)) return FQ_ERR_CUDA;
   const float* plogp = nullptr;
   if (const fq_status st = launch_entries(t, M, V, L, ws, g.entry, g.prob, plogp, s)) return st;
   g.status = reinterpret_cast<int32_t*>(ws);
   g.clear = t.logit == nullptr;
+  g.early_a = g.early_b = t.logit != nullptr;   // the entries come first then
   g.scale = 1.f / t.tau;
   g.E = t.K;
   g.V = V;
   g.part = reinterpret_cast<float2*>(ws + L.part);
   g.zt = reinterpret_cast<float*>(ws + L.zt);
-  if (const fq_status st = launch_logits<kLse>(m, g, s)) return st;
-  return launch(head_join_kernel, ceil_div(M, kJoinWarps), 32 * kJoinWarps, 0, s,
+  if (const fq_status st = launch_logits<kLse>(m, g, sms, s)) return st;
+  // a token to a block only where there are few: of 300 tokens the join took 2 us longer that way,
+  // of one 0.6 us less
+  const int rows = M >= 64 ? 8 : 1;
+  return launch(head_join_kernel, ceil_div(M, rows), kJoinThreads, 0, s,
                 static_cast<const float2*>(g.part), 2 * g.NT, M, V, t.given, g.entry, g.prob,
-                static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, loss,
-                lse, g.status) == cudaSuccess
+                static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, rows,
+                loss, lse, g.status) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
@@ -1064,10 +1095,10 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     return st;
   if (!dloss || (!dx && !dW)) return FQ_ERR_INVALID_ARG;
   if (!aligned16(dloss) || !aligned16(dx) || !aligned16(dW)) return FQ_ERR_ALIGNMENT;
-  if (const fq_status st = check_device()) return st;
+  int sms = 0;
+  if (const fq_status st = device_sms(sms)) return st;
   const Ws L = ws_layout(M, d, V, t.K, true);
   char* ws = static_cast<char*>(wsv);
-  const int sms = sm_count();
   auto* status = reinterpret_cast<int32_t*>(ws);
   auto* xc = reinterpret_cast<__nv_bfloat16*>(ws + L.xc);
   auto* ds = reinterpret_cast<__nv_bfloat16*>(ws + L.ds);
@@ -1097,7 +1128,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     {
       GemmArgs g{};
       GemmMaps m{};
-      if (!plan_logits(g, m, xc, Wq, M, Vc, d, sms, 64) ||
+      if (!plan_logits(g, m, xc, Wq, M, Vc, d, sms, kDl) ||
           !make_tmap(&m.out, ds, M, Vc, ldds, 32))
         return FQ_ERR_CUDA;
       g.status = status;
@@ -1110,7 +1141,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.lse = lse;
       g.dloss = dloss;
       g.gscale = t.logit ? t.tau : 1.f;
-      if (const fq_status st = launch_logits<kDl>(m, g, s)) return st;
+      g.early_b = 1;
+      if (const fq_status st = launch_logits<kDl>(m, g, sms, s)) return st;
     }
     GemmArgs g{};
     GemmMaps m{};
@@ -1120,15 +1152,25 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     g.RT = RT;
     g.NT = NT;
     g.KB = static_cast<int>(ceil_div(Vc, kBK));
+    g.early_b = 1;
+    // dx alone of few tokens holds only their rows of ds
+    g.a_rows = dW ? kBM : static_cast<int>(std::min<int64_t>(kBM, round_up(M, 8)));
+    plan_ring(g, kGrad, static_cast<int>(round_up(g.a_rows * kBK * 2, 1024)), kBN / 2 * kBK * 2);
     g.status = status;
     const int RT2 = static_cast<int>(ceil_div(Vc, 2 * kBM));
     if (dx) {
-      // no split of dx longer than half of a pair's share of the work, if there are few tiles
-      const int64_t work = static_cast<int64_t>(RT) * NT * g.KB +
-                           (dW ? static_cast<int64_t>(RT2) * NT * (KBm + kTile) : 0);
-      const int64_t share = std::max<int64_t>(1, work / (sms / 2));
-      const int splits = static_cast<int>(
-          std::min<int64_t>(most, std::max<int64_t>(1, ceil_div(2 * g.KB, share))));
+      // Split few tiles so that the rounds of splits over the pairs take the least time.  Tiles of
+      // dW even the rounds out: then a split need only be short against a pair's share of the work.
+      const int64_t tiles = static_cast<int64_t>(RT) * NT, pairs = std::max(1, sms / 2);
+      const int64_t share = (tiles * g.KB + (dW ? static_cast<int64_t>(RT2) * NT * (KBm + kTile) : 0)) / pairs;
+      int splits = 1;
+      int64_t least = -1;
+      for (int k = 1; k <= most; ++k) {
+        const int64_t one = ceil_div(g.KB, k) + kTile;
+        const int64_t cost = dW ? std::max<int64_t>(0, one - share / 2) * most + k
+                                : ceil_div(tiles * k, pairs) * one;
+        if (least < 0 || cost < least) least = cost, splits = k;
+      }
       g.kbs = static_cast<int>(ceil_div(g.KB, splits));
       g.KS = static_cast<int>(ceil_div(g.KB, g.kbs));
       g.units = RT * NT * g.KS;
@@ -1136,7 +1178,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.slots = !direct;
       g.filled = used;
       used = std::max(used, g.KS);
-      if (!make_tmap(&m.a, ds, M, Vc, ldds, kBM) || !make_tmap(&m.b, Wq, Vc, d, d, kBK) ||
+      if (!make_tmap(&m.a, ds, M, Vc, ldds, g.a_rows) || !make_tmap(&m.b, Wq, Vc, d, d, kBK) ||
           !(direct ? make_tmap(&m.out, dx, M, d, d, 32)
                    : make_slot_tmap(&m.out, slots, used, M, d)))
         return FQ_ERR_CUDA;
@@ -1152,7 +1194,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
                      d, 32))
         return FQ_ERR_CUDA;
     }
-    if (const fq_status st = launch_gemm_cg<kGrad, 2>(m, g, s)) return st;
+    if (const fq_status st = launch_gemm_cg<kGrad, 2>(m, g, sms, s)) return st;
   }
   if (dx && !direct) {
     const int64_t n4 = static_cast<int64_t>(M) * d / 4;

@@ -43,6 +43,9 @@ namespace fq {
 // n_in and n_out positive multiples of 16, ld_words = 4 ceil(n_in / 64) (FQ_ERR_INVALID_ARG /
 // FQ_ERR_ALIGNMENT), bits = 2 (FQ_ERR_UNSUPPORTED).
 fq_status check_packed(const fq_packed* C);
+// The current device's SM count, asked once per device; FQ_ERR_UNSUPPORTED where it is not of
+// compute capability 10.3, FQ_ERR_CUDA where there is none.
+fq_status device_sms(int& sms);
 
 // ---- fq_pack.cu
 // Dense frame operand (rows x cols bf16, row-major, cols % 8 == 0) -> out: ceil(rows/128) x

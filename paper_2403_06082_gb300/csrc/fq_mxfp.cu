@@ -618,18 +618,6 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 bool sizes_ok(int rows, int cols) { return rows > 0 && cols > 0 && cols % 32 == 0; }
 
-fq_status check_device(int& sms) {
-  int dev = 0, major = 0, minor = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-    return FQ_ERR_CUDA;
-  if (major * 10 + minor != 103) return FQ_ERR_UNSUPPORTED;
-  return cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess
-             ? FQ_OK
-             : FQ_ERR_CUDA;
-}
-
 fq_status check_mxfp(const fq_mxfp* q) {
   if (!q || !q->codes || !q->scales || !sizes_ok(q->rows, q->cols)) return FQ_ERR_INVALID_ARG;
   return aligned16(q->codes) && aligned16(q->scales) ? FQ_OK : FQ_ERR_ALIGNMENT;
@@ -803,7 +791,7 @@ fq_status fq_mxfp_quantize(const void* x, int rows, int cols, const fq_mxfp* q,
   if (q->rows != rows || q->cols != cols) return FQ_ERR_INVALID_ARG;
   if (!aligned16(x)) return FQ_ERR_ALIGNMENT;
   int sms = 0;
-  if (const fq_status st = check_device(sms)) return st;
+  if (const fq_status st = device_sms(sms)) return st;
   return quantize(x, *q, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -812,7 +800,7 @@ fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream) {
   if (const fq_status st = check_mxfp(q)) return st;
   if (!aligned16(y)) return FQ_ERR_ALIGNMENT;
   int sms = 0;
-  if (const fq_status st = check_device(sms)) return st;
+  if (const fq_status st = device_sms(sms)) return st;
   const int KB = stages_of(q->cols);
   return launch(mxfp_dequantize_kernel, q_grid(q->rows, KB), kQThreads, 0, 1,
                 reinterpret_cast<cudaStream_t>(stream),
@@ -831,7 +819,7 @@ fq_status fq_mxfp_product(const fq_mxfp* X, const fq_mxfp* W, void* y, int32_t* 
   if (X->cols != W->cols) return FQ_ERR_INVALID_ARG;
   if (!aligned16(y) || (status && reinterpret_cast<uintptr_t>(status) % 4)) return FQ_ERR_ALIGNMENT;
   int sms = 0;
-  if (const fq_status st = check_device(sms)) return st;
+  if (const fq_status st = device_sms(sms)) return st;
   return product(*X, *W, y, status, sms, false, reinterpret_cast<cudaStream_t>(stream));
 }
 
@@ -850,7 +838,7 @@ fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void*
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return FQ_ERR_ALIGNMENT;
   if (ws_bytes < fq_mxfp_workspace_bytes(M, d_in, W->rows)) return FQ_ERR_WORKSPACE;
   int sms = 0;
-  if (const fq_status st = check_device(sms)) return st;
+  if (const fq_status st = device_sms(sms)) return st;
   const Ws L = ws_layout(M, d_in);
   auto* w = static_cast<uint8_t*>(ws);
   const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
