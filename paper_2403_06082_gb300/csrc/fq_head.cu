@@ -80,7 +80,7 @@ struct GemmMaps {
 
 struct GemmArgs {
   int R, N;                   // rows of A, rows of B (columns of the result); kGrad: of dx
-  int bn;                     // columns per tile (kLse: multiple of 16, kDl: of 64, kGrad: kBN)
+  int bn;                     // columns per tile (multiple of 16 CG; kGrad: kBN)
   int RT, NT, KB, KS, kbs, units;
   int R2, RT2, KB2, units2;   // kGrad: the same of dW (columns as dx, no split)
   int equal;                  // kGrad: tiles of dW that take the time of one of dx
@@ -88,6 +88,7 @@ struct GemmArgs {
   int clear;                  // the call's first kernel: clear the status word
   int a_rows;                 // K-major A: rows per copy (fewer than kBM where R is)
   int stages, stage_bytes, b_off;               // ring of operand stages; B's place in one
+  int per, a_block, b_block;  // k blocks per stage (KB, kbs, ... count stages), bytes of one
   int early_a, early_b;       // the operand (of dx) does not depend on the kernel before this one
   // kLse, kDl
   float scale;                // 1 / tau
@@ -100,6 +101,8 @@ struct GemmArgs {
   const float* lse;           // kDl
   const float* dloss;         // kDl
   float gscale;               // kDl: tau
+  __nv_bfloat16* ds;          // kDl: the piece's ds, row pitch ldds
+  int64_t ldds;
   int slots;                  // kGrad: dx goes to fp32 slots [KS][R][N]
   int filled;                 // kGrad: slots that pieces before this one have written: add to them
 };
@@ -300,8 +303,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
     const uint64_t pol_keep = policy_evict_last(), pol_once = policy_evict_first();
     const int bn_cta = p.bn / CG;                   // rows of B of this CTA
-    const uint32_t bytes = static_cast<uint32_t>(p.a_rows * kBK * 2) +
-                           static_cast<uint32_t>(bn_cta) * kBK * 2;
+    const uint32_t bytes =
+        static_cast<uint32_t>((p.a_rows + bn_cta) * kBK * 2 * (MODE == kGrad ? 1 : p.per));
     // the pair's copies count on the first CTA's barriers
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
     int stage = 0;
@@ -328,12 +331,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (is_a && rank == 0) mbar_arrive_expect_tx(&full[stage], CG * bytes);
           uint8_t* dst = smem + stage * p.stage_bytes + (is_a ? 0 : p.b_off);
           const uint32_t bar = full0 + static_cast<uint32_t>(stage) * 8;
-#pragma unroll
-          for (int h = 0; h < (MODE == kGrad ? 2 : 1); ++h) {
-            const int x = mn ? row + 64 * h : kb * kBK, y = mn ? kb * kBK : row;
-            if (CG == 2) tma_load_2d_pair(dst + h * kAtomBytes, tm, bar, x, y, pol);
-            else tma_load_2d(dst + h * kAtomBytes, tm, &full[stage], x, y, pol);
-            if (!mn) break;
+          // kGrad: an MN-major operand is two boxes of 64 rows; else a box per k block (blocks
+          // beyond the last one arrive as zeros)
+          const int boxes = MODE == kGrad ? (mn ? 2 : 1) : p.per;
+          const int block = MODE == kGrad ? kAtomBytes : (is_a ? p.a_block : p.b_block);
+          const int k = kb * kBK * (MODE == kGrad ? 1 : p.per);
+          for (int h = 0; h < boxes; ++h) {
+            const int x = mn ? row + 64 * h : k + kBK * h, y = mn ? k : row;
+            if (CG == 2) tma_load_2d_pair(dst + h * block, tm, bar, x, y, pol);
+            else tma_load_2d(dst + h * block, tm, &full[stage], x, y, pol);
           }
         }
         if (++stage == p.stages) stage = 0, phase ^= 1;
@@ -366,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t ad0 = amn ? umma_desc_mn(sa) : umma_desc_sw128(sa);
         const uint64_t bd0 = bmn ? umma_desc_mn(sb) : umma_desc_sw128(sb);
         for (int ka = u.k0; ok && ka < u.k1;) {
-          const int ke = MODE == kLse ? min(u.k1, ka + kSegBlocks) : u.k1;
+          const int ke = MODE == kLse ? min(u.k1, ka + kSegBlocks / p.per) : u.k1;
           ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
           if (!ok) break;
           tc_fence_after_sync();
@@ -381,6 +387,15 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < kBK / 16; ++k)
                 umma_cg<CG>(d, ad + k * stepA, bd + k * stepB, idesc,
                             (kb > ka || k > 0) ? 1u : 0u);
+              if (MODE != kGrad) {
+                for (int h = 1; h < p.per; ++h) {
+                  const uint64_t ah = ad + static_cast<uint32_t>(h * p.a_block >> 4);
+                  const uint64_t bh = bd + static_cast<uint32_t>(h * p.b_block >> 4);
+#pragma unroll
+                  for (int k = 0; k < kBK / 16; ++k)
+                    umma_cg<CG>(d, ah + k * stepA, bh + k * stepB, idesc, 1u);
+                }
+              }
               umma_commit_cg<CG>(&empty[stage]);
             }
             if (++stage == p.stages) stage = 0, phase ^= 1;
@@ -446,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int q = 0; q < kHalf; ++q) acc[q] = 0.f;
         bool ok = true;
-        for (int ka = 0; ka < p.KB; ka += kSegBlocks) {
+        for (int ka = 0; ka < p.KB; ka += kSegBlocks / p.per) {
           ok = wait_acc();
           if (!ok) break;
           const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
@@ -506,9 +521,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!wait_acc()) break;
         const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
         const bool rows_any = row_w < p.R;
+        const bool boxed = p.bn % 64 == 0;        // else narrow tiles: rows stored as they are
 #pragma unroll 1
         for (int c = 0; rows_any && c < cols; c += 64) {
-          stage_begin();
+          if (boxed) stage_begin();
 #pragma unroll
           for (int cc = 0; cc < 64; cc += kChunk) {
             float v[kChunk];
@@ -525,15 +541,21 @@ __global__ void __launch_bounds__(kThreads, 1)
               w.step();
             }
 #pragma unroll
-            for (int q = 0; q < kChunk; q += 8)
-              stage_chunk((cc + q) / 8, has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u,
-                          has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u,
-                          has ? pack_bf16(g * v[q + 4], g * v[q + 5]) : 0u,
-                          has ? pack_bf16(g * v[q + 6], g * v[q + 7]) : 0u);
+            for (int q = 0; q < kChunk; q += 8) {
+              const uint32_t o0 = has ? pack_bf16(g * v[q], g * v[q + 1]) : 0u;
+              const uint32_t o1 = has ? pack_bf16(g * v[q + 2], g * v[q + 3]) : 0u;
+              const uint32_t o2 = has ? pack_bf16(g * v[q + 4], g * v[q + 5]) : 0u;
+              const uint32_t o3 = has ? pack_bf16(g * v[q + 6], g * v[q + 7]) : 0u;
+              if (boxed)
+                stage_chunk((cc + q) / 8, o0, o1, o2, o3);
+              else if (row_ok && c + cc + q < h1 - h0)   // not the next tile's columns
+                *reinterpret_cast<uint4*>(p.ds + lrow * p.ldds + n0 + c + cc + q) =
+                    make_uint4(o0, o1, o2, o3);
+            }
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (elect_one()) {
+          if (boxed && elect_one()) {
             tma_store_2d(&maps.out, out, n0 + c, row_w);
             bulk_commit();
           }
@@ -612,14 +634,21 @@ __device__ __forceinline__ bool entry_counts(int32_t index, float logit, int V) 
   return index >= 0 && index < V && !(logit == -CUDART_INF_F);
 }
 
+// x's row of a token without a target is cleared in the copy that the gradients read, so that what
+// it holds (infinities, NaN) meets no product with its zero gradient.
+__device__ __forceinline__ void copy_row(const uint4* x, uint4* xc, int64_t row, int d8, bool has) {
+  for (int j = threadIdx.x; j < d8; j += blockDim.x)
+    xc[row * d8 + j] = has ? __ldcg(x + row * d8 + j) : make_uint4(0u, 0u, 0u, 0u);
+}
+
 // One block per token: the teacher's probabilities of its entries, in ascending order of the
 // vocabulary entry (rank of each entry by counting, K <= 1024), entries that do not count last;
-// and sum_k p_k log p_k.
+// and sum_k p_k log p_k.  For the gradient (xc) also the copy of x.
 constexpr int kSortThreads = 128;
 
 __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
     const int32_t* index, const float* logit, int K, int V, float inv_tau, int32_t* entry,
-    float* prob, float* plogp, int32_t* status) {
+    float* prob, float* plogp, const uint4* x, int d8, uint4* xc, int32_t* status) {
   __shared__ int32_t idx[FQ_DISTILL_MAX_K];
   __shared__ float tl[FQ_DISTILL_MAX_K];
   __shared__ float red[kSortThreads / 32];
@@ -630,17 +659,20 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   float top = -CUDART_INF_F;
+  bool any = false;
   for (int k = threadIdx.x; k < K; k += kSortThreads) {
     const int32_t i = __ldcg(index + base + k);
     const float t = __ldcg(logit + base + k);
     const bool ok = entry_counts(i, t, V);
+    any |= ok;
     idx[k] = ok ? i : kNone;
     tl[k] = ok ? t * inv_tau : -CUDART_INF_F;
     top = fmaxf(top, tl[k]);
   }
   top = warp_max(top);
   if (lane == 0) red[warp] = top;
-  __syncthreads();
+  any = __syncthreads_or(any);
+  if (xc) copy_row(x, xc, blockIdx.x, d8, any);
   top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   __syncthreads();
   const float ref = top == -CUDART_INF_F ? 0.f : top;
@@ -739,20 +771,15 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(
   }
 }
 
-// Copy of x with the rows of tokens without a target cleared, so that what such a row holds
-// (infinities, NaN) meets no product with its zero gradient.  One block per token.  Clears
-// *status where it is the call's first kernel (else null).
-__global__ void __launch_bounds__(256) head_mask_rows_kernel(const uint4* x, int d8,
-                                                             const int32_t* entry, int E, int V,
-                                                             uint4* xc, int32_t* status) {
+// The copy of x where the target is all there is to prepare (cross entropy).  One block per token.
+__global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int d8,
+                                                        const int32_t* target, int V, uint4* xc,
+                                                        int32_t* status) {
   pdl_wait();
   pdl_launch_dependents();                        // as in head_entries_kernel
-  if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
-  const int64_t row = blockIdx.x;
-  const int32_t first = __ldcg(entry + row * E);
-  const bool has = first >= 0 && first < V;
-  for (int j = threadIdx.x; j < d8; j += blockDim.x)
-    xc[row * d8 + j] = has ? __ldcg(x + row * d8 + j) : make_uint4(0u, 0u, 0u, 0u);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
+  const int32_t first = __ldcg(target + blockIdx.x);
+  copy_row(x, xc, blockIdx.x, d8, first >= 0 && first < V);
 }
 
 // dx from its fp32 slots, added in slot order.
@@ -884,7 +911,7 @@ fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, int sms, cudaStre
   cfg.gridDim = dim3(static_cast<unsigned>(std::min(g.units + g.units2, clusters) * CG));
   cfg.blockDim = dim3(kThreads);
   // the MMA reads kBM rows of A, of which a stage may hold fewer: the last stage's too lie inside
-  const int last = (g.stages - 1) * g.stage_bytes + kABytes;
+  const int last = (g.stages - 1) * g.stage_bytes + (g.per - 1) * g.a_block + kABytes;
   cfg.dynamicSmemBytes = static_cast<size_t>(
       1024 + std::max(last, g.stages * g.stage_bytes + out_bytes(MODE) + kTailBytes));
   cfg.stream = s;
@@ -928,9 +955,18 @@ int64_t most_tiles(int R, int N) {
   return std::max<int64_t>(ceil_div(N, kBN), kMaxSms / cg / ceil_div(R, kBM * cg));
 }
 
+// The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
+// cycles whatever it holds, so narrow tiles take up to four blocks of k at a time (32 KiB at most).
 void plan_ring(GemmArgs& g, int mode, int a_bytes, int b_bytes) {
-  g.b_off = a_bytes;
-  g.stage_bytes = a_bytes + b_bytes;
+  g.per = 1;
+  while (mode != kGrad && g.per < 4 && g.per < g.KB &&
+         (a_bytes + b_bytes) * g.per * 2 <= 32 * 1024)
+    g.per *= 2;
+  g.a_block = a_bytes;
+  g.b_block = b_bytes;
+  g.KB = static_cast<int>(ceil_div(g.KB, g.per));
+  g.b_off = a_bytes * g.per;
+  g.stage_bytes = (a_bytes + b_bytes) * g.per;
   g.stages = std::min(kMaxStages,
                       (kSmemMost - (mode == kLse ? kRoom : 0) - 1024 - kTailBytes - out_bytes(mode)) /
                           g.stage_bytes);
@@ -942,7 +978,7 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
   const int cg = group_for(R);
   g.R = R;
   g.N = N;
-  g.bn = pick_bn(R, N, sms, mode == kDl ? 64 : 16 * cg);
+  g.bn = pick_bn(R, N, sms, 16 * cg);
   g.RT = static_cast<int>(ceil_div(R, kBM * cg));
   g.NT = static_cast<int>(ceil_div(N, g.bn));
   g.KB = g.kbs = static_cast<int>(ceil_div(d, kBK));
@@ -952,6 +988,7 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
   // copies, or nothing yet) does not matter
   g.a_rows = static_cast<int>(std::min<int64_t>(kBM, round_up(R, 8)));
   plan_ring(g, mode, static_cast<int>(round_up(g.a_rows * kBK * 2, 1024)), g.bn / cg * kBK * 2);
+  g.kbs = g.KB;
   return make_tmap(&m.a, x, R, d, d, g.a_rows) && make_tmap(&m.b, W, N, d, d, g.bn / cg);
 }
 
@@ -1029,25 +1066,30 @@ fq_status check_common(const void* x, int M, int d, const void* W, int V, const 
   return FQ_OK;
 }
 
-// The token's entries in ascending order: the target itself, or the sorted teacher's list.
-fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws,
-                         const int32_t*& entry, const float*& prob, const float*& plogp,
+// The token's entries in ascending order: the target itself, or the sorted teacher's list; with xc,
+// the copy of x.
+fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, const void* x, int d,
+                         void* xc, const int32_t*& entry, const float*& prob, const float*& plogp,
                          cudaStream_t s) {
+  auto* status = reinterpret_cast<int32_t*>(ws);
+  const auto* x4 = static_cast<const uint4*>(x);
+  auto* xc4 = static_cast<uint4*>(xc);
+  cudaError_t e = cudaSuccess;
   if (!t.logit) {
     entry = t.given;
     prob = plogp = nullptr;
-    return FQ_OK;
+    if (xc) e = launch(head_copy_kernel, M, 256, 0, s, x4, d / 8, t.given, V, xc4, status);
+  } else {
+    auto* en = reinterpret_cast<int32_t*>(ws + L.entry);
+    auto* pr = reinterpret_cast<float*>(ws + L.prob);
+    auto* pl = reinterpret_cast<float*>(ws + L.plogp);
+    entry = en;
+    prob = pr;
+    plogp = pl;
+    e = launch(head_entries_kernel, M, kSortThreads, 0, s, t.given, t.logit, t.K, V, 1.f / t.tau,
+               en, pr, pl, x4, d / 8, xc4, status);
   }
-  auto* e = reinterpret_cast<int32_t*>(ws + L.entry);
-  auto* pr = reinterpret_cast<float*>(ws + L.prob);
-  auto* pl = reinterpret_cast<float*>(ws + L.plogp);
-  entry = e;
-  prob = pr;
-  plogp = pl;
-  return launch(head_entries_kernel, M, kSortThreads, 0, s, t.given, t.logit, t.K, V,
-                1.f / t.tau, e, pr, pl, reinterpret_cast<int32_t*>(ws)) == cudaSuccess
-             ? FQ_OK
-             : FQ_ERR_CUDA;
+  return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
 fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Target& t,
@@ -1065,7 +1107,9 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   GemmMaps m{};
   if (!plan_logits(g, m, x, W, M, V, d, sms, kLse)) return FQ_ERR_CUDA;
   const float* plogp = nullptr;
-  if (const fq_status st = launch_entries(t, M, V, L, ws, g.entry, g.prob, plogp, s)) return st;
+  if (const fq_status st =
+          launch_entries(t, M, V, L, ws, x, d, nullptr, g.entry, g.prob, plogp, s))
+    return st;
   g.status = reinterpret_cast<int32_t*>(ws);
   g.clear = t.logit == nullptr;
   g.early_a = g.early_b = t.logit != nullptr;   // the entries come first then
@@ -1107,10 +1151,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
 
   const int32_t* entry = nullptr;
   const float *prob = nullptr, *plogp = nullptr;
-  if (const fq_status st = launch_entries(t, M, V, L, ws, entry, prob, plogp, s)) return st;
-  if (launch(head_mask_rows_kernel, M, 256, 0, s, static_cast<const uint4*>(x), d / 8, entry, t.K,
-             V, reinterpret_cast<uint4*>(xc), t.logit ? nullptr : status) != cudaSuccess)
-    return FQ_ERR_CUDA;
+  if (const fq_status st = launch_entries(t, M, V, L, ws, x, d, xc, entry, prob, plogp, s))
+    return st;
 
   const int P = piece_width(M, V);
   const int pieces = static_cast<int>(ceil_div(V, P));
@@ -1141,6 +1183,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.lse = lse;
       g.dloss = dloss;
       g.gscale = t.logit ? t.tau : 1.f;
+      g.ds = ds;
+      g.ldds = ldds;
       g.early_b = 1;
       if (const fq_status st = launch_logits<kDl>(m, g, sms, s)) return st;
     }
