@@ -937,22 +937,31 @@ fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStrea
                              : launch_gemm_cg<MODE, 1>(m, g, sms, s);
 }
 
-// Columns per tile of the logit products, a multiple of `unit`.  A tile's time hardly depends on
-// its width (19.4 us at 128 columns and 23.0 us at 256 for d = 4096, CG = 2), so tiles are as wide
-// as they go, unless all of them fit the SMs (or pairs) at once: then they are as narrow as still
-// does.
-int pick_bn(int R, int N, int sms, int unit) {
-  const int cg = group_for(R);
+// Columns per tile of the logit products, a multiple of 16 CG.  All tiles at once on the SMs (or
+// pairs): as narrow as still does.  Else the width whose rounds take the least time, where a
+// round goes as its width + 64 columns for up to 128 tokens (which stream W: 39654 x 2440 for 16
+// tokens 51 us at 256 columns and two rounds, 46 at 144 and two, 51 at 128 and three) and + 256
+// for more (2048 tokens, 32000 x 4096: 20.3 us a round at 256 columns, 15.7 at 128).
+constexpr int kMinBn = 64;                      // where there are several rounds
+
+int pick_bn(int R, int N, int sms) {
+  const int cg = group_for(R), unit = 16 * cg;
   const int64_t RT = ceil_div(R, kBM * cg), room = std::min(sms, kMaxSms) / cg;
-  int bn = kBN;
-  while (bn > unit && RT * ceil_div(N, bn - unit) <= room) bn -= unit;
-  return bn;
+  int best = kBN;
+  int64_t least = -1;
+  for (int bn = kBN; bn >= unit; bn -= unit) {
+    const int64_t rounds = ceil_div(RT * ceil_div(N, bn), room);
+    if (bn < kMinBn && rounds > 1) break;
+    const int64_t cost = rounds * (bn + (cg == 1 ? 64 : 256));
+    if (least < 0 || cost < least) least = cost, best = bn;
+  }
+  return best;
 }
 
 // Most column tiles of the logit products on any device.
 int64_t most_tiles(int R, int N) {
   const int cg = group_for(R);
-  return std::max<int64_t>(ceil_div(N, kBN), kMaxSms / cg / ceil_div(R, kBM * cg));
+  return std::max<int64_t>(ceil_div(N, kMinBn), kMaxSms / cg / ceil_div(R, kBM * cg));
 }
 
 // The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
@@ -978,7 +987,7 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
   const int cg = group_for(R);
   g.R = R;
   g.N = N;
-  g.bn = pick_bn(R, N, sms, 16 * cg);
+  g.bn = pick_bn(R, N, sms);
   g.RT = static_cast<int>(ceil_div(R, kBM * cg));
   g.NT = static_cast<int>(ceil_div(N, g.bn));
   g.KB = g.kbs = static_cast<int>(ceil_div(d, kBK));
@@ -994,7 +1003,7 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
 
 constexpr int64_t kPieceBytes = 128ll << 20;    // ds of one piece of the vocabulary
 constexpr int kMinPiece = 2048;
-constexpr int kMaxSlots = 16;                   // fp32 slots of a dx split over the vocabulary
+constexpr int kMaxSlots = 32;                   // fp32 slots of a dx split over the vocabulary
 
 // Vocabulary entries per piece: as many as kPieceBytes of ds hold (at least kMinPiece), in
 // pieces of equal size rounded up to 256.
