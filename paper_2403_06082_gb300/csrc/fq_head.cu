@@ -457,51 +457,87 @@ __global__ void __launch_bounds__(kThreads, 1)
       if constexpr (MODE == kLse) {
         const bool row_ok = row < p.R;
         const int64_t lrow = row_ok ? row : 0;
-        float acc[kHalf];
-#pragma unroll
-        for (int q = 0; q < kHalf; ++q) acc[q] = 0.f;
-        bool ok = true;
-        for (int ka = 0; ka < p.KB; ka += kSegBlocks / p.per) {
-          ok = wait_acc();
-          if (!ok) break;
-          const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
-#pragma unroll
-          for (int c = 0; c < kHalf; c += 16) {
-            float v[16];
-            tmem_ld16(t_row + c, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[c + q] += v[q];
-          }
-          release_acc();
-        }
-        if (!ok) break;
-        EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, n0);
         const float c2 = p.scale * kLog2e;
         float m = -CUDART_INF_F, sum = 0.f;       // maximum and sum, in units of log 2
+        if (p.KB * p.per <= kSegBlocks) {
+          // one accumulator holds the whole sum: 32 columns at a time
+          EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, n0);
+          if (!wait_acc()) break;
+          const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
+#pragma unroll 1
+          for (int c = 0; c < cols; c += kChunk) {
+            float x[kChunk];
+            __syncwarp();
+            tmem_ld32(t_row + c, x);
+            tmem_wait_ld();
+            while (w.next < n0 + min(c + kChunk, cols)) {
+              const int j = w.next - (n0 + c);
+              float z = 0.f;
 #pragma unroll
-        for (int c = 0; c < kHalf; c += kChunk) {
-          while (w.next < n0 + min(c + kChunk, cols)) {
-            const int j = w.next - (n0 + c);
-            float z = 0.f;
+              for (int q = 0; q < kChunk; ++q) z = q == j ? x[q] : z;
+              p.zt[lrow * p.E + w.k] = z * p.scale;
+              w.step();
+            }
+            float mx[4] = {m, m, m, m};
 #pragma unroll
-            for (int q = 0; q < kChunk; ++q) z = q == j ? acc[c + q] : z;
-            p.zt[lrow * p.E + w.k] = z * p.scale;
-            w.step();
+            for (int q = 0; q < kChunk; ++q) {
+              x[q] = c + q < cols ? x[q] * c2 : -CUDART_INF_F;
+              mx[q & 3] = fmaxf(mx[q & 3], x[q]);
+            }
+            const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            const float ref = mn == -CUDART_INF_F ? 0.f : mn;
+            float sx[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) sx[q & 3] += ex2(x[q] - ref);
+            sum = fmaf(sum, ex2(m - ref), (sx[0] + sx[1]) + (sx[2] + sx[3]));
+            m = mn;
           }
+          release_acc();
+        } else {
+          float acc[kHalf];
 #pragma unroll
-          for (int q = 0; q < kChunk; ++q) {
-            acc[c + q] = c + q < cols ? acc[c + q] * c2 : -CUDART_INF_F;
-            m = fmaxf(m, acc[c + q]);
+          for (int q = 0; q < kHalf; ++q) acc[q] = 0.f;
+          bool ok = true;
+          for (int ka = 0; ka < p.KB; ka += kSegBlocks / p.per) {
+            ok = wait_acc();
+            if (!ok) break;
+            const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
+#pragma unroll
+            for (int c = 0; c < kHalf; c += 16) {
+              float v[16];
+              tmem_ld16(t_row + c, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int q = 0; q < 16; ++q) acc[c + q] += v[q];
+            }
+            release_acc();
           }
-        }
-        const float ref = m == -CUDART_INF_F ? 0.f : m;
+          if (!ok) break;
+          EntryWalk w(p.entry + lrow * p.E, row_ok ? p.E : 0, n0);
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 8) {
-          float s = 0.f;
+          for (int c = 0; c < kHalf; c += kChunk) {
+            while (w.next < n0 + min(c + kChunk, cols)) {
+              const int j = w.next - (n0 + c);
+              float z = 0.f;
 #pragma unroll
-          for (int q = 0; q < 8; ++q) s += ex2(acc[c + q] - ref);
-          sum += s;
+              for (int q = 0; q < kChunk; ++q) z = q == j ? acc[c + q] : z;
+              p.zt[lrow * p.E + w.k] = z * p.scale;
+              w.step();
+            }
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) {
+              acc[c + q] = c + q < cols ? acc[c + q] * c2 : -CUDART_INF_F;
+              m = fmaxf(m, acc[c + q]);
+            }
+          }
+          const float ref = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+          for (int c = 0; c < kHalf; c += 8) {
+            float sx = 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sx += ex2(acc[c + q] - ref);
+            sum += sx;
+          }
         }
         if (row_ok)
           p.part[(static_cast<int64_t>(u.col / p.bn) * 2 + half) * p.R + row] = make_float2(m, sum);
@@ -701,7 +737,7 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
 }
 
 // Joins the tiles' maxima and sums of each token, then the loss; reports targets beyond the
-// vocabulary.  A block takes `rows` tokens (1 or 8): neighbouring
+// vocabulary.  A block takes `rows` tokens (1, 2, 4 or 8): neighbouring
 // lanes are neighbouring tokens, and the 256 / rows threads of a token share its tiles and its
 // entries.  Parts are joined in a fixed order.
 constexpr int kJoinThreads = 256;
@@ -717,8 +753,7 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r = lane & (rows - 1);
-  const int g = rows == 1 ? static_cast<int>(threadIdx.x) : static_cast<int>(threadIdx.x) >> 3;
-  const int groups = rows == 1 ? kJoinThreads : kJoinThreads / 8;
+  const int g = static_cast<int>(threadIdx.x) / rows, groups = kJoinThreads / rows;
   const int row = blockIdx.x * rows + r;
   const bool ok = row < M;
   const int64_t base = static_cast<int64_t>(ok ? row : 0) * E;
@@ -1128,9 +1163,9 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   g.part = reinterpret_cast<float2*>(ws + L.part);
   g.zt = reinterpret_cast<float*>(ws + L.zt);
   if (const fq_status st = launch_logits<kLse>(m, g, sms, s)) return st;
-  // a token to a block only where there are few: of 300 tokens the join took 2 us longer that way,
-  // of one 0.6 us less
-  const int rows = M >= 64 ? 8 : 1;
+  // Eight tokens to a block, fewer where they have many tiles, one where there are few tokens: of
+  // 300 tokens with 64 tiles the join took 2 us longer with a block for each, of one 0.6 us less.
+  const int rows = M < 64 ? 1 : g.NT <= 64 ? 8 : g.NT <= 128 ? 4 : 2;
   return launch(head_join_kernel, ceil_div(M, rows), kJoinThreads, 0, s,
                 static_cast<const float2*>(g.part), 2 * g.NT, M, V, t.given, g.entry, g.prob,
                 static_cast<const float*>(g.zt), plogp, t.K, t.logit ? t.tau * t.tau : 1.f, rows,
@@ -1212,16 +1247,22 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     g.status = status;
     const int RT2 = static_cast<int>(ceil_div(Vc, 2 * kBM));
     if (dx) {
-      // Split few tiles so that the rounds of splits over the pairs take the least time.  Tiles of
-      // dW even the rounds out: then a split need only be short against a pair's share of the work.
+      // Split few tiles so that they take the least time, in k blocks (about 0.27 us): the rounds of
+      // splits over the pairs, or with tiles of dW, which even the rounds out, a pair's share of
+      // the work but no less than one split; the slots' way to memory and back (at 5 TB/s); and
+      // the kernel that adds the slots up.
       const int64_t tiles = static_cast<int64_t>(RT) * NT, pairs = std::max(1, sms / 2);
-      const int64_t share = (tiles * g.KB + (dW ? static_cast<int64_t>(RT2) * NT * (KBm + kTile) : 0)) / pairs;
+      const int64_t share =
+          (tiles * g.KB + (dW ? static_cast<int64_t>(RT2) * NT * (KBm + kTile) : 0)) / pairs;
+      const double slot = 6e-6 * M * d;
+      constexpr int kAdd = 12;
       int splits = 1;
-      int64_t least = -1;
+      double least = -1;
       for (int k = 1; k <= most; ++k) {
         const int64_t one = ceil_div(g.KB, k) + kTile;
-        const int64_t cost = dW ? std::max<int64_t>(0, one - share / 2) * most + k
-                                : ceil_div(tiles * k, pairs) * one;
+        const double cost =
+            static_cast<double>(dW ? std::max(one, share) : ceil_div(tiles * k, pairs) * one) +
+            (k > 1 ? k * slot + kAdd : 0);
         if (least < 0 || cost < least) least = cost, splits = k;
       }
       g.kbs = static_cast<int>(ceil_div(g.KB, splits));
