@@ -1000,11 +1000,11 @@ int64_t most_tiles(int R, int N) {
 }
 
 // The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
-// cycles whatever it holds, so narrow tiles take up to four blocks of k at a time (32 KiB at most).
+// cycles whatever it holds, so narrow tiles take up to four blocks of k at a time (44 KiB at most).
 void plan_ring(GemmArgs& g, int mode, int a_bytes, int b_bytes) {
   g.per = 1;
   while (mode != kGrad && g.per < 4 && g.per < g.KB &&
-         (a_bytes + b_bytes) * g.per * 2 <= 32 * 1024)
+         (a_bytes + b_bytes) * g.per * 2 <= 44 * 1024)
     g.per *= 2;
   g.a_block = a_bytes;
   g.b_block = b_bytes;
