@@ -1,0 +1,155 @@
+"""What quantization costs a small model, and how distillation wins some of it back.
+
+The model is one linear layer and an output weight over a vocabulary: h = x W1^T, logits =
+h W2^T, with the 256 x 256 layer and the activations of the `single256` workload and a random
+output weight.  It is the teacher.  Its layer is then held in three ways:
+
+  2-bit frame coefficients   fq_pack, rebuilt as one weight by fq_reconstruct_weight
+  4-bit microscaled floats   fq_mxfp_quantize, run by fq_mxfp_linear
+  bf16                       fq_dense_forward
+
+and each is scored by the cross entropy of tokens drawn from the teacher (fq_cross_entropy, as a
+perplexity evaluation does, without the logits).  The 2-bit student's output weight is then
+trained on the teacher's top logits (fq_distill, fq_distill_grad) with plain gradient steps.
+
+    python examples/score_and_recover.py [--tokens 2048] [--vocabulary 5003] [--steps 40]
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+import numpy as np  # noqa: E402
+import torch  # noqa: E402
+
+import paper_2403_06082_gb300 as fq  # noqa: E402
+import workloads as wl  # noqa: E402
+
+BF16 = torch.bfloat16
+RHO = wl.RHO
+
+
+def scratch(n, dev):
+    return torch.zeros(n, dtype=torch.uint8, device=dev)
+
+
+def frame_quantized(W, d, dev):
+    """The d x d layer in 2-bit frame coefficients, rebuilt as one bf16 weight."""
+    wk = wl.WORKLOADS["single256"]
+    k = wk.fixed_k
+    n = k * RHO
+
+    def frame(side):
+        r = wl.rotation_draws(wk.seed, wk.key, "single", side, d=d)
+        nb = fq.fq_frame_workspace_bytes(k, RHO, d, r.a, r.b)
+        T = torch.empty(n, d, device=dev)
+        fq.fq_frame_build(k, RHO, d, (r.a, r.b, r.ga, r.gb, r.perm, r.signs), T,
+                          scratch(nb, dev), nb)
+        return T
+
+    T_in, T_out = frame("in"), frame("out")
+    C = torch.empty(n, n, device=dev)
+    nb = fq.fq_coefficients_workspace_bytes(d, n)
+    fq.fq_coefficients(W, d, d, T_in, n, T_out, n, C, scratch(nb, dev), nb)
+    codes = torch.empty(n, n, dtype=torch.uint8, device=dev)
+    scale, zero = (torch.empty(n, dtype=torch.int16, device=dev) for _ in range(2))
+    gamma = torch.empty(n, device=dev)
+    fq.fq_quantize_rtn(C, n, n, codes, scale, zero, gamma)
+    words = torch.empty(fq.fq_packed_words(n, n), dtype=torch.int32, device=dev)
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    packed = fq.fq_pack(codes, scale, zero, n, n, words, status)
+    assert fq.fq_check(status) == 0
+    nb = fq.fq_reconstruct_workspace_bytes(d, n, n, d)
+    ws = scratch(nb, dev)
+    W_hat = torch.empty(d, d, dtype=BF16, device=dev)
+    fq.fq_reconstruct_weight(T_in.to(BF16), packed, T_out.t().contiguous().to(BF16), d, d, gamma,
+                             W_hat, ws, nb)
+    assert fq.fq_check(ws) == 0
+    return W_hat
+
+
+def dense(x, W):
+    M, d, d_out = x.shape[0], x.shape[1], W.shape[0]
+    y = torch.empty(M, d_out, dtype=BF16, device=x.device)
+    nb = fq.fq_dense_workspace_bytes(M, d, d_out)
+    ws = scratch(nb, x.device)
+    fq.fq_dense_forward(x, M, d, W, d_out, y, ws, nb)
+    assert fq.fq_check(ws) == 0
+    return y
+
+
+def microscaled(x, W):
+    M, d, d_out = x.shape[0], x.shape[1], W.shape[0]
+    q = fq.fq_mxfp_alloc(d_out, d)
+    fq.fq_mxfp_quantize(W, d_out, d, q)
+    y = torch.empty(M, d_out, dtype=BF16, device=x.device)
+    nb = fq.fq_mxfp_workspace_bytes(M, d, d_out)
+    ws = scratch(nb, x.device)
+    fq.fq_mxfp_linear(x, M, d, q, y, ws, nb)
+    assert fq.fq_check(ws) == 0
+    return y
+
+
+def main(argv=None):
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--tokens", type=int, default=2048)
+    ap.add_argument("--vocabulary", type=int, default=5003)
+    ap.add_argument("--steps", type=int, default=40)
+    ap.add_argument("--rate", type=float, default=0.01)
+    a = ap.parse_args(argv)
+    dev = torch.device("cuda:0")
+    M, V, K, tau = a.tokens, a.vocabulary, 32, 2.0
+    wk = wl.WORKLOADS["single256"]
+    layer = wk.layers[0]
+    d = layer.d_in
+    g = torch.Generator(device=dev).manual_seed(0)
+
+    W1 = torch.from_numpy(wl.weight(wk, layer)).to(dev, torch.float32)
+    x = torch.from_numpy(wl.activations(wk, layer, M)).to(dev, BF16)
+    W2 = (torch.randn(V, d, generator=g, device=dev) * 0.1).to(BF16)
+    hidden = {"bf16": dense(x, W1.to(BF16)), "2-bit frames": dense(x, frame_quantized(W1, d, dev)),
+              "4-bit microscaled": microscaled(x, W1.to(BF16))}
+
+    # what the teacher says: tokens drawn from it to be scored on, and its top logits to learn
+    logits = hidden["bf16"].float() @ W2.float().T
+    target = torch.multinomial(torch.softmax(logits, 1), 1, generator=g)[:, 0].to(torch.int32)
+    top, index = logits.topk(K, 1)
+    top, index = top.contiguous(), index.to(torch.int32).contiguous()
+    del logits
+
+    nb = max(fq.fq_head_workspace_bytes(M, d, V, K), fq.fq_head_grad_workspace_bytes(M, d, V, K))
+    ws = scratch(nb, dev)
+    loss, lse = torch.empty(M, device=dev), torch.empty(M, device=dev)
+
+    def score(h, W):
+        fq.fq_cross_entropy(h, M, d, W, V, target, loss, lse, ws, nb)
+        assert fq.fq_check(ws) == 0
+        return float(loss.double().mean())
+
+    out = {"scores": {name: score(h, W2) for name, h in hidden.items()}}
+    for name, v in out["scores"].items():
+        print(f"{name:18s} cross entropy {v:.4f}, perplexity {np.exp(v):.1f}")
+
+    # the 2-bit student learns a new output weight from the teacher
+    h = hidden["2-bit frames"]
+    master = W2.float()
+    dW = torch.empty_like(W2)
+    dloss = torch.full((M,), 1.0 / M, device=dev)
+    out["distill"] = []
+    for step in range(a.steps):
+        W = master.to(BF16)
+        fq.fq_distill(h, M, d, W, V, index, top, K, tau, loss, lse, ws, nb)
+        fq.fq_distill_grad(h, M, d, W, V, index, top, K, tau, lse, dloss, None, dW, ws, nb)
+        out["distill"].append(float(loss.mean()))
+        master -= a.rate * dW.float()
+    out["recovered"] = score(h, master.to(BF16))
+    print(f"distillation loss {out['distill'][0]:.4f} -> {out['distill'][-1]:.4f} in {a.steps} "
+          f"steps; 2-bit frames now {out['recovered']:.4f}")
+    return out
+
+
+if __name__ == "__main__":
+    main()

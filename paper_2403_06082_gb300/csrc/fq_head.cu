@@ -976,7 +976,8 @@ fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStrea
 // pairs): as narrow as still does.  Else the width whose rounds take the least time, where a
 // round goes as its width + 64 columns for up to 128 tokens (which stream W: 39654 x 2440 for 16
 // tokens 51 us at 256 columns and two rounds, 46 at 144 and two, 51 at 128 and three) and + 256
-// for more (2048 tokens, 32000 x 4096: 20.3 us a round at 256 columns, 15.7 at 128).
+// for up to 512 (256 tokens, 32000 x 4096: 27.3 us a round at 256 columns, 18.9 at 128).  More
+// tokens have so many tiles that the widest are best (2048 tokens: 285 us at 256, 288 at 224).
 constexpr int kMinBn = 64;                      // where there are several rounds
 
 int pick_bn(int R, int N, int sms) {
@@ -986,7 +987,7 @@ int pick_bn(int R, int N, int sms) {
   int64_t least = -1;
   for (int bn = kBN; bn >= unit; bn -= unit) {
     const int64_t rounds = ceil_div(RT * ceil_div(N, bn), room);
-    if (bn < kMinBn && rounds > 1) break;
+    if (rounds > 1 && bn < (RT <= 2 ? kMinBn : kBN)) break;
     const int64_t cost = rounds * (bn + (cg == 1 ? 64 : 256));
     if (least < 0 || cost < least) least = cost, best = bn;
   }
@@ -996,7 +997,8 @@ int pick_bn(int R, int N, int sms) {
 // Most column tiles of the logit products on any device.
 int64_t most_tiles(int R, int N) {
   const int cg = group_for(R);
-  return std::max<int64_t>(ceil_div(N, kMinBn), kMaxSms / cg / ceil_div(R, kBM * cg));
+  const int64_t RT = ceil_div(R, kBM * cg);
+  return std::max<int64_t>(ceil_div(N, RT <= 2 ? kMinBn : kBN), kMaxSms / cg / RT);
 }
 
 // The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
