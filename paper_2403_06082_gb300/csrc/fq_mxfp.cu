@@ -28,6 +28,11 @@
 // KS CTAs splits the k range of one tile and adds the parts up, in rank order, through
 // distributed shared memory.
 //
+// Up to 16 tokens the product takes bf16 x itself (FUSE): each CTA's epilogue warps quantise its k
+// range of x into shared memory, for all of its tiles, while W's first stages arrive.  One launch
+// instead of two; the range is bounded by kFuseStages and kFuseValues, beyond which every CTA
+// quantising the same x costs more than a kernel that does it once.
+//
 // Warp roles: warp 0 producer of W's codes, warp 1 TMEM owner + MMA issuer (of the first CTA of a
 // pair), warps 2-9 epilogue (thread = accumulator row, half of the tokens), warps 10-17 scales,
 // warp 18 producer of X's codes.
@@ -59,7 +64,12 @@ constexpr int kSlots = 5;
 constexpr int kAhead = 2;                       // of its stages that a group of scale warps holds
 static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 
-constexpr int kNumBars = 2 * kMaxStages + 4;
+constexpr int kNumBars = 2 * kMaxStages + 5;
+constexpr int kFuseTokens = 16;
+constexpr int kFuseStages = 32;                 // FUSE: k range of a CTA, in stages
+constexpr int kFuseValues = 16 * 1024;          // FUSE: tokens x k range of a CTA
+constexpr int kXBlock = kFuseTokens * kKStage / 2;            // FUSE: x's codes of a stage
+constexpr int kXScales = kFuseTokens * kKStage / 32;          // FUSE: and their scales
 constexpr int kTailBytes = kNumBars * 8 + 16;
 constexpr int kSmemMost = 227 * 1024;
 
@@ -67,9 +77,9 @@ constexpr int kSmemMost = 227 * 1024;
 __host__ __device__ constexpr int stage_bytes(int bn_cta) {
   return kABytes + bn_cta * (kKStage / 2);
 }
-int stages_for(int bn_cta) {
+int stages_for(int bytes, int reserved) {
   // at least kSlots: a slot of scales then never waits for a later round of its stage
-  return std::min(kMaxStages, (kSmemMost - kTailBytes - 1024) / stage_bytes(bn_cta));
+  return std::min(kMaxStages, (kSmemMost - kTailBytes - 1024 - reserved) / bytes);
 }
 
 struct ProdArgs {
@@ -82,6 +92,9 @@ struct ProdArgs {
   const uint8_t* sx;
   int wgroups, xgroups;       // row groups of W's and of X's scales
   int early_w;                // W does not depend on the kernel before this one
+  const uint4* x;             // FUSE: bf16 M x K
+  int K;
+  int x_bytes;                // FUSE: shared memory of x's codes and scales
   __nv_bfloat16* y;
   int32_t* status;
 };
@@ -130,20 +143,56 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
   return v;
 }
 
-template <int CG, bool SPLIT>
+// Two values to E2M1 codes: to nearest, ties to the even code, saturating; hi in bits 4-7.
+__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 t;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
+      "cvt.u32.u8 %0, t;\n\t}"
+      : "=r"(r)
+      : "f"(lo), "f"(hi));
+  return r;
+}
+
+// Codes of this thread's 8 values and the scale of the block of 32 that it shares with its three
+// neighbours (four lanes from a multiple of four on; a whole warp calls).
+__device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t& scale) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t m2 = 0;                                // largest magnitudes of even and odd values
+#pragma unroll
+  for (int q = 0; q < 4; ++q) m2 = __vmaxu2(m2, w[q] & 0x7fff7fffu);
+  m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
+  m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
+  const uint32_t ex = max(m2 & 0xffffu, m2 >> 16) >> 7;
+  const bool fine = ex != 255;                    // no infinity and no NaN
+  scale = fine ? (ex > 2 ? ex - 2 : 0) : 255u;
+  // 2^(127 - scale): the multiplication is exact, or far below the first step
+  const float inv = __uint_as_float((254u - min(scale, 252u)) << 23);
+  uint32_t c = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float lo = __uint_as_float(w[q] << 16), hi = __uint_as_float(w[q] & 0xffff0000u);
+    c |= e2m1x2(lo * inv, hi * inv) << (8 * q);
+  }
+  return fine ? c : 0u;
+}
+
+template <int CG, bool SPLIT, bool FUSE>
 __global__ void __launch_bounds__(kThreads, 1)
     mxfp_product_kernel(const __grid_constant__ CUtensorMap tmW,
                         const __grid_constant__ CUtensorMap tmX, const ProdArgs p) {
-  static_assert(CG == 1 || !SPLIT, "a pair does not split its tile's k");
+  static_assert(CG == 1 || (!SPLIT && !FUSE), "a pair does not split its tile's k");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + p.stages * p.stage_bytes);
+  uint8_t* xcodes = smem + p.stages * p.stage_bytes;             // FUSE
+  uint64_t* full = reinterpret_cast<uint64_t*>(xcodes + (FUSE ? p.x_bytes : 0));
   // full: codes of both CTAs in shared memory, scales of both in TMEM (first CTA's barriers);
   // empty: they have been read
   uint64_t* empty = full + kMaxStages;
   uint64_t* tfull = empty + kMaxStages;
   uint64_t* tempty = tfull + 2;                   // used in the pair's first CTA
+  uint64_t* xready = tempty + 2;                  // FUSE: x is quantised
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(full + kNumBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -155,6 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int step = SPLIT ? p.units : static_cast<int>(gridDim.x) / CG;
   const int k0 = SPLIT ? min(p.KB, rank * p.kbs) : 0;
   const int k1 = SPLIT ? min(p.KB, k0 + p.kbs) : p.KB;
+  uint8_t* xscales = xcodes + (FUSE ? (SPLIT ? p.kbs : p.KB) * kXBlock : 0);
   // tile u = row tile * TT + token tile: the CTAs of a wave share W's tiles
   auto tile_n0 = [&](int u) { return u % p.TT * p.bn; };
   // first row group (128 rows) of this CTA's part of W
@@ -171,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&tfull[b], 1);
       mbar_init(&tempty[b], 8 * CG);
     }
+    mbar_init(xready, 8);
     *abort_flag = 0;
     fence_barrier_init();
     prefetch_tmap(&tmW);
@@ -194,12 +245,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     *abort_flag = 1;
   };
 
-  if (warp == 0 || warp == 18) {
+  if (warp == 0 || (!FUSE && warp == 18)) {
     // ---------------------------------------------------------------- producers
     const bool is_w = warp == 0;
     const uint64_t pol = is_w && p.TT == 1 ? policy_evict_first() : policy_evict_last();
     const int bn_cta = p.bn / CG;
-    const uint32_t bytes = static_cast<uint32_t>(kABytes + bn_cta * (kKStage / 2));
+    const uint32_t bytes = static_cast<uint32_t>(kABytes + (FUSE ? 0 : bn_cta * (kKStage / 2)));
     const CUtensorMap* tm = is_w ? &tmW : &tmX;
     // the pair's copies count on the first CTA's barriers
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
@@ -260,6 +311,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       int stage = 0, slot = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
+      const uint64_t xdesc0 = umma_desc_sw128(smem_u32(xcodes));
+      if (FUSE) ok = mbar_wait_warp(xready, 0, abort_flag);
       for (int u = first; ok && k0 < k1 && u < p.units; u += step) {
         ok = mbar_wait_warp(&tempty[buf], acc_phase ^ 1, abort_flag);
         if (!ok) break;
@@ -273,7 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_after_sync();
           const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + slot * kSfCols);
           const uint64_t ad = desc0 + static_cast<uint32_t>(stage * p.stage_bytes >> 4);
-          const uint64_t bd = ad + (kABytes >> 4);
+          const uint64_t bd = FUSE ? xdesc0 + static_cast<uint32_t>((kb - k0) * (kXBlock >> 4))
+                                   : ad + (kABytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)        // 64 k = 32 bytes along a row per step
@@ -290,6 +344,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) timed_out();
     }
+  } else if (FUSE && warp == 18) {
+    // x has no producer
   } else if (warp >= 10 && warp < 18) {
     // ---------------------------------------------------------------- scales
     // A slot's TMEM columns: W's two tiles of 4 blocks, then X's (8 columns each).
@@ -308,13 +364,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       // a pair's second half may lie beyond the last row group: its rows are not used
       const int rg = min(tile_rg(q.u), p.wgroups - 1), n0 = tile_n0(q.u);
       q.w = p.sw + (static_cast<int64_t>(rg) * p.KB + q.kb) * kSfBytes + lane * 16;
-      q.x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
-      q.two = groups_of(n0) > 1;
+      if (!FUSE) q.x = p.sx + (static_cast<int64_t>(n0 / 128) * p.KB + q.kb) * kSfBytes + lane * 16;
+      q.two = !FUSE && groups_of(n0) > 1;
     };
     auto skip = [&]() {
       if (++q.kb < k1) {
         q.w += kSfBytes;
-        q.x += kSfBytes;
+        if (!FUSE) q.x += kSfBytes;
       } else {
         q.kb = k0;
         q.u += step;
@@ -332,13 +388,23 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
         h.v[a] = __ldcg(reinterpret_cast<const uint4*>(q.w + a * 512));
-        h.v[2 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + a * 512));
+        if (FUSE) {
+          // this lane's token, in the first of its tile's four columns; the others are not used
+          const uint32_t w = lane < kFuseTokens
+                                 ? *reinterpret_cast<const uint32_t*>(
+                                       xscales + (q.kb - k0) * kXScales + lane * 8 + a * 4)
+                                 : 0u;
+          h.v[2 + a] = make_uint4(w, 0u, 0u, 0u);
+        } else {
+          h.v[2 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + a * 512));
+        }
         if (q.two) h.v[4 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + next_group + a * 512));
       }
       skip();
       skip();
     };
     pdl_wait();
+    bool ok = !FUSE || mbar_wait_warp(xready, 0, abort_flag), more = ok;
     enter();
     if (group) skip();
 #pragma unroll
@@ -349,7 +415,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t parity = 1;                           // of a phase before the first: passes
     if (before >= p.stages) before -= p.stages, parity ^= 1;
     const uint32_t full0 = CG == 2 ? mapa(smem_u32(full), 0) : 0u;
-    bool ok = true, more = true;
     while (more) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
@@ -388,6 +453,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int hw = (p.bn / 2 + 15) / 16 * 16;
     const int h0 = half * hw, h1 = half ? p.bn : hw;
     pdl_wait();
+    if (FUSE) {
+      // codes as TMA would leave them: 16 rows of 128 bytes a stage under the 128-byte swizzle
+      const int per_token = (k1 - k0) * (kKStage / 8);            // threads of a token
+      const int d8 = p.K / 8, first8 = k0 * (kKStage / 8);
+      const int n = p.M * per_token;                              // a multiple of 32
+      for (int i0 = threadIdx.x - 64; i0 < n; i0 += 4 * 256) {
+        uint4 v[4];                                               // four loads in flight
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = i0 + q * 256, t = i / per_token, j = i % per_token;
+          v[q] = make_uint4(0u, 0u, 0u, 0u);
+          if (i < n && first8 + j < d8) v[q] = __ldcg(p.x + static_cast<int64_t>(t) * d8 + first8 + j);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = i0 + q * 256, t = i / per_token, j = i % per_token;
+          if (i >= n) break;
+          uint32_t sc;
+          const uint32_t c = quantise8(v[q], sc);
+          const int st = j / 32, in = j % 32;
+          *reinterpret_cast<uint32_t*>(xcodes + st * kXBlock + t * 128 +
+                                       ((in / 4 ^ (t & 7)) << 4) + in % 4 * 4) = c;
+          if (in % 4 == 0) xscales[st * kXScales + t * 8 + in / 4] = static_cast<uint8_t>(sc);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(xready);
+    }
     int buf = 0;
     uint32_t acc_phase = 0;
     for (int u = first; u < p.units; u += step) {
@@ -463,17 +557,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 // ---------------------------------------------------------------------------------------------
 // quantisation
 // ---------------------------------------------------------------------------------------------
-// Two values to E2M1 codes: to nearest, ties to the even code, saturating; hi in bits 4-7.
-__device__ __forceinline__ uint32_t e2m1x2(float lo, float hi) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 t;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
-      "cvt.u32.u8 %0, t;\n\t}"
-      : "=r"(r)
-      : "f"(lo), "f"(hi));
-  return r;
-}
-
 // A block of threads covers 8 x 4 rows by one stage of 256 columns: a warp is a row of 256 values
 // (8 a thread), and a thread has the rows r, r + 32, r + 64, r + 96 of a group of 128, so that its
 // four loads are in flight together and their scales, which lie side by side, move as 16 bytes.
@@ -513,26 +596,11 @@ __global__ void __launch_bounds__(kQThreads) mxfp_quantize_kernel(const uint4* x
   uint32_t words[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-    uint32_t m2 = 0;                              // largest magnitudes of even and odd values
-#pragma unroll
-    for (int q = 0; q < 4; ++q) m2 = __vmaxu2(m2, w[q] & 0x7fff7fffu);
-    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 1));
-    m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, 2));
-    const uint32_t ex = max(m2 & 0xffffu, m2 >> 16) >> 7;
-    const bool fine = ex != 255;                  // no infinity and no NaN
-    const uint32_t sc = fine ? (ex > 2 ? ex - 2 : 0) : 255u;
-    // 2^(127 - sc): the multiplication is exact, or far below the first step
-    const float inv = __uint_as_float((254u - min(sc, 252u)) << 23);
-    uint32_t c = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float lo = __uint_as_float(w[q] << 16), hi = __uint_as_float(w[q] & 0xffff0000u);
-      c |= e2m1x2(lo * inv, hi * inv) << (8 * q);
-    }
+    uint32_t sc;
+    const uint32_t c = quantise8(v[j], sc);
     const int row = at.row + 32 * j;
     if (in_col && row < rows)
-      codes[static_cast<int64_t>(row) * (cols / 8) + at.block] = fine ? c : 0u;
+      codes[static_cast<int64_t>(row) * (cols / 8) + at.block] = c;
     // four blocks' scales as one word
     uint32_t word = sc << (8 * (threadIdx.x >> 2 & 3));
     word |= __shfl_xor_sync(0xffffffffu, word, 4);
@@ -658,7 +726,7 @@ fq_status quantize(const void* x, const fq_mxfp& q, cudaStream_t s) {
 }
 
 // CTAs (CG = 2: pairs) that the device runs at once.
-template <int CG, bool SPLIT>
+template <int CG, bool SPLIT, bool FUSE>
 fq_status prepare_product(int sms, int& room) {
   static std::mutex mu;
   static std::map<int, int> fit;
@@ -667,7 +735,7 @@ fq_status prepare_product(int sms, int& room) {
   std::lock_guard<std::mutex> lock(mu);
   auto it = fit.find(dev);
   if (it == fit.end()) {
-    if (cudaFuncSetAttribute(mxfp_product_kernel<CG, SPLIT>,
+    if (cudaFuncSetAttribute(mxfp_product_kernel<CG, SPLIT, FUSE>,
                              cudaFuncAttributeMaxDynamicSharedMemorySize,
                              kSmemMost) != cudaSuccess)
       return FQ_ERR_CUDA;
@@ -685,7 +753,7 @@ fq_status prepare_product(int sms, int& room) {
       cfg.attrs = attr;
       cfg.numAttrs = 1;
       int most = 0;
-      if (cudaOccupancyMaxActiveClusters(&most, mxfp_product_kernel<CG, SPLIT>, &cfg) !=
+      if (cudaOccupancyMaxActiveClusters(&most, mxfp_product_kernel<CG, SPLIT, FUSE>, &cfg) !=
               cudaSuccess ||
           most < 1)
         return FQ_ERR_CUDA;
@@ -697,14 +765,14 @@ fq_status prepare_product(int sms, int& room) {
   return FQ_OK;
 }
 
-template <int CG, bool SPLIT>
+template <int CG, bool SPLIT, bool FUSE>
 fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProdArgs& a, int sms,
                          cudaStream_t s) {
   int room = 0;
-  if (const fq_status st = prepare_product<CG, SPLIT>(sms, room)) return st;
+  if (const fq_status st = prepare_product<CG, SPLIT, FUSE>(sms, room)) return st;
   const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room) * CG;
-  return launch(mxfp_product_kernel<CG, SPLIT>, dim3(static_cast<unsigned>(grid)), kThreads,
-                static_cast<size_t>(a.stages) * a.stage_bytes + kTailBytes + 1024, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
+  return launch(mxfp_product_kernel<CG, SPLIT, FUSE>, dim3(static_cast<unsigned>(grid)), kThreads,
+                static_cast<size_t>(a.stages) * a.stage_bytes + a.x_bytes + kTailBytes + 1024, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
@@ -724,36 +792,73 @@ int pick_bn(int M, int R, int sms) {
   return cost(128) < cost(192) ? 128 : 192;
 }
 
-fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, int sms,
-                  bool early_w, cudaStream_t s) {
+// The tiles of M tokens and W, and the split of k.
+ProdArgs plan_product(int M, const fq_mxfp& W, int sms, int& cg) {
   ProdArgs a{};
   a.R = W.rows;
-  a.M = X.rows;
+  a.M = M;
+  a.K = W.cols;
   a.bn = pick_bn(a.M, a.R, sms);
   a.TT = static_cast<int>(ceil_div(a.M, a.bn));
   // pairs of CTAs once their tiles fill the SMs
-  const int cg = ceil_div(a.R, 2 * kBM) * a.TT >= sms / 2 ? 2 : 1;
+  cg = ceil_div(a.R, 2 * kBM) * a.TT >= sms / 2 ? 2 : 1;
   a.RT = static_cast<int>(ceil_div(a.R, cg * kBM));
   a.KB = stages_of(W.cols);
   a.units = a.RT * a.TT;
   a.KS = 1;
   while (cg == 1 && a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
   a.kbs = static_cast<int>(ceil_div(a.KB, a.KS));
-  a.stages = stages_for(a.bn / cg);
-  a.stage_bytes = stage_bytes(a.bn / cg);
   a.sw = W.scales;
-  a.sx = X.scales;
   a.wgroups = static_cast<int>(ceil_div(a.R, 128));
   a.xgroups = static_cast<int>(ceil_div(a.M, 128));
+  return a;
+}
+
+fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, int sms,
+                  bool early_w, cudaStream_t s) {
+  int cg = 1;
+  ProdArgs a = plan_product(X.rows, W, sms, cg);
+  a.stage_bytes = stage_bytes(a.bn / cg);
+  a.stages = stages_for(a.stage_bytes, 0);
+  a.sx = X.scales;
   a.early_w = early_w;
   a.y = static_cast<__nv_bfloat16*>(y);
   a.status = status;
   CUtensorMap mw, mx;
-  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM) || !make_tmap(&mx, X.codes, X.rows, X.cols, a.bn / cg))
+  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM) ||
+      !make_tmap(&mx, X.codes, X.rows, X.cols, a.bn / cg))
     return FQ_ERR_CUDA;
-  if (cg == 2) return launch_product<2, false>(mw, mx, a, sms, s);
-  return a.KS > 1 ? launch_product<1, true>(mw, mx, a, sms, s)
-                  : launch_product<1, false>(mw, mx, a, sms, s);
+  if (cg == 2) return launch_product<2, false, false>(mw, mx, a, sms, s);
+  return a.KS > 1 ? launch_product<1, true, false>(mw, mx, a, sms, s)
+                  : launch_product<1, false, false>(mw, mx, a, sms, s);
+}
+
+// The product of bf16 x, quantised on the way; false where x is too large for that.
+bool fused_product(const void* x, int M, const fq_mxfp& W, void* y, int32_t* status, int sms,
+                   cudaStream_t s, fq_status& st) {
+  if (M > kFuseTokens) return false;
+  int cg = 1;
+  ProdArgs a = plan_product(M, W, sms, cg);
+  const int range = a.KS > 1 ? a.kbs : a.KB;
+  if (range > kFuseStages || M * range * kKStage > kFuseValues) return false;
+  if (cg == 2) {                                  // tiles of one CTA: W is what is read
+    a.RT = static_cast<int>(ceil_div(a.R, kBM));
+    a.units = a.RT * a.TT;
+  }
+  a.x_bytes = range * (kXBlock + kXScales);
+  a.stage_bytes = kABytes;
+  a.stages = stages_for(a.stage_bytes, a.x_bytes);
+  a.x = static_cast<const uint4*>(x);
+  a.y = static_cast<__nv_bfloat16*>(y);
+  a.status = status;
+  CUtensorMap mw;
+  if (!make_tmap(&mw, W.codes, W.rows, W.cols, kBM)) {
+    st = FQ_ERR_CUDA;
+    return true;
+  }
+  st = a.KS > 1 ? launch_product<1, true, true>(mw, mw, a, sms, s)
+                : launch_product<1, false, true>(mw, mw, a, sms, s);
+  return true;
 }
 
 struct Ws {
@@ -843,8 +948,11 @@ fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void*
   auto* w = static_cast<uint8_t*>(ws);
   const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
   auto s = reinterpret_cast<cudaStream_t>(stream);
-  if (const fq_status st = quantize(x, X, s)) return st;
-  return product(X, *W, y, static_cast<int32_t*>(ws), sms, true, s);
+  auto* status = static_cast<int32_t*>(ws);
+  fq_status st = FQ_OK;
+  if (fused_product(x, M, *W, y, status, sms, s, st)) return st;
+  if ((st = quantize(x, X, s)) != FQ_OK) return st;
+  return product(X, *W, y, status, sms, true, s);
 }
 
 }  // extern "C"

@@ -105,6 +105,24 @@ def test_linear(M, d, V):
     assert (over <= 0).all(), (float(over.max()), int(over.argmax()))
 
 
+@pytest.mark.parametrize("M,d,V", [
+    (1, 8192, 300), (1, 8224, 300), (2, 8192, 28672), (8, 2048, 40000), (16, 1024, 130),
+    (16, 1056, 130), (3, 5472, 200), (4, 4096, 4096), (5, 4096, 4096), (1, 32, 20000)])
+def test_linear_of_few_tokens(M, d, V):
+    """Sizes about the bounds between quantising x on the way and ahead of the product: the same
+    bits as the product of the quantised x, whichever way it goes."""
+    x, w = _matrix(M, d, 11), _matrix(V, d, 12, loud=False)
+    q = _quantised(w)
+    y = _linear(x, w, q)
+    two = torch.empty_like(y)
+    fq.fq_mxfp_product(_quantised(x), q, two)
+    assert torch.equal(y, two)
+    if V * d <= 1 << 22:
+        X, W = dequantised(x).to(DEV), dequantised(w).to(DEV)
+        ref = X @ W.T
+        assert ((y.double() - ref).abs() <= _bound(X, W, ref)).all()
+
+
 @pytest.mark.parametrize("M", [3, 300])
 def test_product_of_two_quantised_is_the_linear(M):
     x, w = _matrix(M, 1024, 3), _matrix(500, 1024, 4, loud=False)
@@ -115,7 +133,7 @@ def test_product_of_two_quantised_is_the_linear(M):
     assert torch.equal(y, _linear(x, w))
 
 
-@pytest.mark.parametrize("M", [4, 260])
+@pytest.mark.parametrize("M", [4, 20, 260])
 def test_a_nan_block_shows_where_it_takes_part_and_nowhere_else(M):
     x, w = _matrix(M, 512, 5), _matrix(300, 512, 6, loud=False)
     clean = _linear(x, w)
