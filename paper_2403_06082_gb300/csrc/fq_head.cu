@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t sa = smem_u32(smem), sb = sa + static_cast<uint32_t>(p.b_off);
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;             // ready: the next stage was seen to be full
       Unit u;
       for (int i = 0; ok && unit_at<MODE, CG>(p, cid, ncl, i, u); ++i) {
         const bool amn = MODE == kGrad && u.w;
@@ -378,9 +378,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_after_sync();
           const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kBN);
           for (int kb = ka; kb < ke; ++kb) {
-            ok = mbar_wait_warp(&full[stage], phase, abort_flag);
-            if (!ok) break;
-            const uint32_t at = static_cast<uint32_t>(stage * p.stage_bytes) >> 4;
+            if (!__all_sync(0xffffffffu, ready)) {
+              ok = mbar_wait_warp(&full[stage], phase, abort_flag);
+              if (!ok) break;
+            }
+            const int now = stage;
+            if (++stage == p.stages) stage = 0, phase ^= 1;
+            ready = mbar_test_wait(&full[stage], phase);
+            const uint32_t at = static_cast<uint32_t>(now * p.stage_bytes) >> 4;
             const uint64_t ad = ad0 + at, bd = bd0 + at;
             if (elect_one()) {
 #pragma unroll
@@ -396,9 +401,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     umma_cg<CG>(d, ah + k * stepA, bh + k * stepB, idesc, 1u);
                 }
               }
-              umma_commit_cg<CG>(&empty[stage]);
+              umma_commit_cg<CG>(&empty[now]);
             }
-            if (++stage == p.stages) stage = 0, phase ^= 1;
           }
           if (!ok) break;
           if (elect_one()) umma_commit_cg<CG>(&tfull[buf]);
@@ -1261,7 +1265,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       int splits = 1;
       double least = -1;
       for (int k = 1; k <= most; ++k) {
-        const int64_t one = ceil_div(g.KB, k) + kTile;
+        // (with one row tile W comes from memory at that moment: twice the time)
+        const int64_t one = (RT == 1 ? 2 : 1) * ceil_div(g.KB, k) + kTile;
         const double cost =
             static_cast<double>(dW ? std::max(one, share) : ceil_div(tiles * k, pairs) * one) +
             (k > 1 ? k * slot + kAdd : 0);

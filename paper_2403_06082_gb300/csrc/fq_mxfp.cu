@@ -99,12 +99,23 @@ struct ProdArgs {
   int32_t* status;
 };
 
-// A lane's 16 bytes of 512 bytes of scales (rows l, l + 32, l + 64, l + 96, four each) -> 4 TMEM
-// columns of this warp's lane quarter.
-__device__ __forceinline__ void sf_store(uint32_t tmem, const uint4& v) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tmem),
-               "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-               : "memory");
+// A lane holds 16 bytes of every 512 bytes of scales (rows l, l + 32, l + 64, l + 96, four each):
+// 4 TMEM columns of this warp's lane quarter.  Two of them to 8 columns, four to 16.
+__device__ __forceinline__ void sf_store8(uint32_t tmem, const uint4& a, const uint4& b) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(tmem),
+      "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+      : "memory");
+}
+
+__device__ __forceinline__ void sf_store16(uint32_t tmem, const uint4& a, const uint4& b,
+                                           const uint4& c, const uint4& d) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, "
+      "%9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(tmem),
+      "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w), "r"(c.x),
+      "r"(c.y), "r"(c.z), "r"(c.w), "r"(d.x), "r"(d.y), "r"(d.z), "r"(d.w)
+      : "memory");
 }
 
 // Instruction descriptor, kind::mxf4: E2M1 A and B (1), power-of-two scales (bit 23), fp32
@@ -310,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t desc0 = umma_desc_sw128(smem_u32(smem));
       int stage = 0, slot = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;             // ready: the next stage was seen to be full
       const uint64_t xdesc0 = umma_desc_sw128(smem_u32(xcodes));
       if (FUSE) ok = mbar_wait_warp(xready, 0, abort_flag);
       for (int u = first; ok && k0 < k1 && u < p.units; u += step) {
@@ -321,11 +332,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         // X's rows start at n0: its scales (n0 mod 128) / 32 columns into their tile
         const uint32_t shift = 8 + static_cast<uint32_t>(tile_n0(u) % 128) / 32;
         for (int kb = k0; kb < k1; ++kb) {
-          ok = mbar_wait_warp(&full[stage], phase, abort_flag);
-          if (!ok) break;
+          if (!__all_sync(0xffffffffu, ready)) {
+            ok = mbar_wait_warp(&full[stage], phase, abort_flag);
+            if (!ok) break;
+          }
           tc_fence_after_sync();
+          const int now = stage;
+          if (++stage == p.stages) stage = 0, phase ^= 1;
+          ready = mbar_test_wait(&full[stage], phase);
           const uint32_t tsf = tmem_base + static_cast<uint32_t>(kSfCol + slot * kSfCols);
-          const uint64_t ad = desc0 + static_cast<uint32_t>(stage * p.stage_bytes >> 4);
+          const uint64_t ad = desc0 + static_cast<uint32_t>(now * p.stage_bytes >> 4);
           const uint64_t bd = FUSE ? xdesc0 + static_cast<uint32_t>((kb - k0) * (kXBlock >> 4))
                                    : ad + (kABytes >> 4);
           if (elect_one()) {
@@ -333,9 +349,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 4; ++j)        // 64 k = 32 bytes along a row per step
               umma_mxf4<CG>(d, ad + 2 * j, bd + 2 * j, j & 1 ? id2 : id0, tsf + (j >> 1) * 4,
                             tsf + shift + (j >> 1) * 8, (kb > k0 || j > 0) ? 1u : 0u);
-            umma_commit_cg<CG>(&empty[stage]);
+            umma_commit_cg<CG>(&empty[now]);
           }
-          if (++stage == p.stages) stage = 0, phase ^= 1;
           if (++slot == kSlots) slot = 0;
         }
         if (!ok) break;
@@ -379,12 +394,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     struct Held {
       uint4 v[6];
-      bool any, two;
+      bool any;
     } held[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) held[i].v[4] = held[i].v[5] = make_uint4(0u, 0u, 0u, 0u);
     auto fetch = [&](Held& h) {
       h.any = k0 < k1 && q.u < p.units;
       if (!h.any) return;
-      h.two = q.two;
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
         h.v[a] = __ldcg(reinterpret_cast<const uint4*>(q.w + a * 512));
@@ -426,12 +442,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t t = t_sf + static_cast<uint32_t>(slot * kSfCols);
-#pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          sf_store(t + a * 4, held[i].v[a]);
-          sf_store(t + 8 + a * 8, held[i].v[2 + a]);
-          if (held[i].two) sf_store(t + 12 + a * 8, held[i].v[4 + a]);
-        }
+        // (a second row group that is not there leaves what it held: its tokens are not used)
+        sf_store8(t, held[i].v[0], held[i].v[1]);
+        sf_store16(t + 8, held[i].v[2], held[i].v[4], held[i].v[3], held[i].v[5]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before_sync();
         __syncwarp();
