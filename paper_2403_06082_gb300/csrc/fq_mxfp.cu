@@ -403,7 +403,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!h.any) return;
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
-        h.v[a] = __ldcg(reinterpret_cast<const uint4*>(q.w + a * 512));
+        // through L1: the four warps of a group read the same bytes, and past it these would be
+        // a third of a stage's traffic from L2
+        h.v[a] = *reinterpret_cast<const uint4*>(q.w + a * 512);
         if (FUSE) {
           // this lane's token, in the first of its tile's four columns; the others are not used
           const uint32_t w = lane < kFuseTokens
@@ -412,9 +414,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  : 0u;
           h.v[2 + a] = make_uint4(w, 0u, 0u, 0u);
         } else {
-          h.v[2 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + a * 512));
+          h.v[2 + a] = *reinterpret_cast<const uint4*>(q.x + a * 512);
         }
-        if (q.two) h.v[4 + a] = __ldcg(reinterpret_cast<const uint4*>(q.x + next_group + a * 512));
+        if (q.two) h.v[4 + a] = *reinterpret_cast<const uint4*>(q.x + next_group + a * 512);
       }
       skip();
       skip();
