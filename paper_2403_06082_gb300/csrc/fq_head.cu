@@ -13,9 +13,14 @@
 // A token is a row of the accumulator in kLse and kDl, i.e. one epilogue thread per half row, so
 // the softmax statistics need no exchange between threads.  Operands whose contraction dimension
 // is not the contiguous one (W for dx, ds and x for dW) are read as they lie in memory, as
-// MN-major tiles: nothing is transposed.  ds is rounded to bf16, the type that the tensor cores
-// multiply with bf16 W and x: it adds 2^-9 of each entry, of either sign, to gradients that are
-// rounded to bf16 themselves.
+// MN-major tiles: nothing is transposed.
+//
+// ds is rounded to bf16, the type that the tensor cores multiply with bf16 W and x.  What is
+// rounded is ds over a reference dloss, which the results are multiplied by in fp32: with the usual
+// dloss of 1 / tokens the target's entry of an unsure token is then -1 + q, close to an exact
+// value, where -1 / tokens would be off by the same 2^-9 or less for every token alike (gradients
+// of 4096 tokens were off by 2.2e-3 to 2.5e-3 of their norm that way, by where 1 / tokens fell
+// between two bf16 values; rounding the results alone is 1.7e-3).
 //
 // With CG = 2 a cluster of two CTAs works on one tile of 256 x bn: each CTA stages its 128 rows
 // of A and half of the rows of B, one MMA reads both CTAs' shared memory, and each CTA finishes
@@ -100,7 +105,8 @@ struct GemmArgs {
   float* zt;                  // kLse: [R][E] logits (over tau) of the entries
   const float* lse;           // kDl
   const float* dloss;         // kDl
-  float gscale;               // kDl: tau
+  const float* gref;          // kDl, kGrad: the reference dloss
+  float gscale;               // kGrad: tau
   __nv_bfloat16* ds;          // kDl: the piece's ds, row pitch ldds
   int64_t ldds;
   int slots;                  // kGrad: dx goes to fp32 slots [KS][R][N]
@@ -451,6 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto stage_chunk = [&](int c, uint32_t a, uint32_t b, uint32_t d, uint32_t e) {
       *reinterpret_cast<uint4*>(out + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(a, b, d, e);
     };
+    const float gout = MODE == kGrad ? __ldcg(p.gref) * p.gscale : 1.f;
     Unit u;
     for (int i = 0; unit_at<MODE, CG>(p, cid, ncl, i, u); ++i) {
       const int row_w = u.row + rank * kBM + quarter * 32;        // first row of the warp
@@ -556,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int first = __ldcg(p.entry + lrow * p.E);
           has = first >= 0 && first < p.V;
           lse2 = __ldcg(p.lse + row) * kLog2e;
-          g = __ldcg(p.dloss + row) * p.gscale;
+          g = __ldcg(p.dloss + row) / __ldcg(p.gref);
         }
         if (!wait_acc()) break;
         const uint32_t t_row = t_lane + static_cast<uint32_t>(buf * kBN);
@@ -613,6 +620,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           float v[32];
           tmem_ld32(t_row + c, v);
           tmem_wait_ld();
+#pragma unroll
+          for (int q = 0; q < 32; ++q) v[q] *= gout;
           if (wide) {
 #pragma unroll
             for (int q = 0; q < 32; q += 4)
@@ -625,6 +634,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                           pack_bf16(v[q + 4], v[q + 5]), pack_bf16(v[q + 6], v[q + 7]));
             tmem_ld32(t_row + c + 32, v);
             tmem_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) v[q] *= gout;
 #pragma unroll
             for (int q = 0; q < 32; q += 8)
               stage_chunk(4 + q / 8, pack_bf16(v[q], v[q + 1]), pack_bf16(v[q + 2], v[q + 3]),
@@ -681,14 +692,35 @@ __device__ __forceinline__ void copy_row(const uint4* x, uint4* xc, int64_t row,
     xc[row * d8 + j] = has ? __ldcg(x + row * d8 + j) : make_uint4(0u, 0u, 0u, 0u);
 }
 
+// The reference dloss: that of the first token with a target, or 1 where there is none or it is
+// no ordinary number.  One block.
+template <typename HasTarget>
+__device__ __forceinline__ void find_reference(int M, const float* dloss, float* gref,
+                                               HasTarget has) {
+  __shared__ int first;
+  if (threadIdx.x == 0) first = kNone;
+  __syncthreads();
+  for (int base = 0; base < M; base += blockDim.x) {
+    const int i = base + static_cast<int>(threadIdx.x);
+    const bool hit = i < M && has(i);
+    if (hit) atomicMin(&first, i);
+    if (__syncthreads_or(hit)) break;             // the block leaves as one
+  }
+  if (threadIdx.x == 0) {
+    const float g = first == kNone ? 1.f : __ldcg(dloss + first);
+    *gref = fabsf(g) >= 1e-18f && fabsf(g) <= 1e18f ? g : 1.f;
+  }
+}
+
 // One block per token: the teacher's probabilities of its entries, in ascending order of the
 // vocabulary entry (rank of each entry by counting, K <= 1024), entries that do not count last;
-// and sum_k p_k log p_k.  For the gradient (xc) also the copy of x.
+// and sum_k p_k log p_k.  For the gradient (xc) also the copy of x, and the reference dloss.
 constexpr int kSortThreads = 128;
 
 __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
     const int32_t* index, const float* logit, int K, int V, float inv_tau, int32_t* entry,
-    float* prob, float* plogp, const uint4* x, int d8, uint4* xc, int32_t* status) {
+    float* prob, float* plogp, int M, const uint4* x, int d8, uint4* xc, const float* dloss,
+    float* gref, int32_t* status) {
   __shared__ int32_t idx[FQ_DISTILL_MAX_K];
   __shared__ float tl[FQ_DISTILL_MAX_K];
   __shared__ float red[kSortThreads / 32];
@@ -738,6 +770,14 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   if (lane == 0) red[warp] = h;
   __syncthreads();
   if (threadIdx.x == 0) plogp[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+  if (xc && blockIdx.x == 0)
+    find_reference(M, dloss, gref, [&](int i) {
+      for (int k = 0; k < K; ++k)
+        if (entry_counts(__ldcg(index + static_cast<int64_t>(i) * K + k),
+                         __ldcg(logit + static_cast<int64_t>(i) * K + k), V))
+          return true;
+      return false;
+    });
 }
 
 // Joins the tiles' maxima and sums of each token, then the loss; reports targets beyond the
@@ -810,15 +850,22 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(
   }
 }
 
-// The copy of x where the target is all there is to prepare (cross entropy).  One block per token.
-__global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int d8,
+// The copy of x and the reference dloss where the target is all there is to prepare (cross
+// entropy).  One block per token.
+__global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int M, int d8,
                                                         const int32_t* target, int V, uint4* xc,
+                                                        const float* dloss, float* gref,
                                                         int32_t* status) {
   pdl_wait();
   pdl_launch_dependents();                        // as in head_entries_kernel
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
   const int32_t first = __ldcg(target + blockIdx.x);
   copy_row(x, xc, blockIdx.x, d8, first >= 0 && first < V);
+  if (blockIdx.x == 0)
+    find_reference(M, dloss, gref, [&](int i) {
+      const int32_t t = __ldcg(target + i);
+      return t >= 0 && t < V;
+    });
 }
 
 // dx from its fp32 slots, added in slot order.
@@ -1063,7 +1110,7 @@ int most_splits(int M, int d, int Vc, int sms) {
 }
 
 struct Ws {
-  size_t entry, prob, plogp, zt, part, xc, ds, slots, total;
+  size_t entry, prob, plogp, gref, zt, part, xc, ds, slots, total;
 };
 
 Ws ws_layout(int M, int d, int V, int K, bool grad) {
@@ -1078,6 +1125,7 @@ Ws ws_layout(int M, int d, int V, int K, bool grad) {
   L.entry = take(mk);
   L.prob = take(mk);
   L.plogp = take(static_cast<size_t>(M) * 4);
+  L.gref = take(4);
   if (!grad) {
     L.zt = take(mk);
     L.part = take(static_cast<size_t>(most_tiles(M, V)) * 2 * M * 8);
@@ -1119,16 +1167,18 @@ fq_status check_common(const void* x, int M, int d, const void* W, int V, const 
 // The token's entries in ascending order: the target itself, or the sorted teacher's list; with xc,
 // the copy of x.
 fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, const void* x, int d,
-                         void* xc, const int32_t*& entry, const float*& prob, const float*& plogp,
+                         void* xc, const float* dloss, const int32_t*& entry, const float*& prob, const float*& plogp,
                          cudaStream_t s) {
   auto* status = reinterpret_cast<int32_t*>(ws);
   const auto* x4 = static_cast<const uint4*>(x);
   auto* xc4 = static_cast<uint4*>(xc);
+  auto* gref = reinterpret_cast<float*>(ws + L.gref);
   cudaError_t e = cudaSuccess;
   if (!t.logit) {
     entry = t.given;
     prob = plogp = nullptr;
-    if (xc) e = launch(head_copy_kernel, M, 256, 0, s, x4, d / 8, t.given, V, xc4, status);
+    if (xc)
+      e = launch(head_copy_kernel, M, 256, 0, s, x4, M, d / 8, t.given, V, xc4, dloss, gref, status);
   } else {
     auto* en = reinterpret_cast<int32_t*>(ws + L.entry);
     auto* pr = reinterpret_cast<float*>(ws + L.prob);
@@ -1137,7 +1187,7 @@ fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, c
     prob = pr;
     plogp = pl;
     e = launch(head_entries_kernel, M, kSortThreads, 0, s, t.given, t.logit, t.K, V, 1.f / t.tau,
-               en, pr, pl, x4, d / 8, xc4, status);
+               en, pr, pl, M, x4, d / 8, xc4, dloss, gref, status);
   }
   return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
@@ -1158,7 +1208,7 @@ fq_status head_loss(const void* x, int M, int d, const void* W, int V, const Tar
   if (!plan_logits(g, m, x, W, M, V, d, sms, kLse)) return FQ_ERR_CUDA;
   const float* plogp = nullptr;
   if (const fq_status st =
-          launch_entries(t, M, V, L, ws, x, d, nullptr, g.entry, g.prob, plogp, s))
+          launch_entries(t, M, V, L, ws, x, d, nullptr, nullptr, g.entry, g.prob, plogp, s))
     return st;
   g.status = reinterpret_cast<int32_t*>(ws);
   g.clear = t.logit == nullptr;
@@ -1201,7 +1251,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
 
   const int32_t* entry = nullptr;
   const float *prob = nullptr, *plogp = nullptr;
-  if (const fq_status st = launch_entries(t, M, V, L, ws, x, d, xc, entry, prob, plogp, s))
+  if (const fq_status st = launch_entries(t, M, V, L, ws, x, d, xc, dloss, entry, prob, plogp, s))
     return st;
 
   const int P = piece_width(M, V);
@@ -1232,7 +1282,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.v0 = v0;
       g.lse = lse;
       g.dloss = dloss;
-      g.gscale = t.logit ? t.tau : 1.f;
+      g.gref = reinterpret_cast<const float*>(ws + L.gref);
       g.ds = ds;
       g.ldds = ldds;
       g.early_b = 1;
@@ -1246,6 +1296,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     g.RT = RT;
     g.NT = NT;
     g.KB = static_cast<int>(ceil_div(Vc, kBK));
+    g.gref = reinterpret_cast<const float*>(ws + L.gref);
+    g.gscale = t.logit ? t.tau : 1.f;
     g.early_b = 1;
     // dx alone of few tokens holds only their rows of ds
     g.a_rows = dW ? kBM : static_cast<int>(std::min<int64_t>(kBM, round_up(M, 8)));

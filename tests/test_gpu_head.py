@@ -111,6 +111,45 @@ def test_distillation_and_gradients(M, d, V, K, tau):
     _hold(_call(s), s)
 
 
+@pytest.mark.parametrize("K", [0, 5])
+@pytest.mark.parametrize("dloss", ["mean", "zero_first", "tiny", "huge", "masked_nan"])
+def test_kinds_of_dloss(K, dloss):
+    """The usual 1 / tokens; a first token of no weight; sizes at the ends of fp32; and what
+    tokens without a target hold, from the first one on."""
+    s = _inputs(300, 128, 700, K, seed=21, tau=2.0)
+    off = (s["target"] < 0) if K == 0 else (s["index"] < 0).all(1)
+    if dloss == "mean":
+        s["dloss"] = torch.full_like(s["dloss"], 1.0 / 271)
+    elif dloss == "zero_first":
+        s["dloss"][:5] = 0.0
+    elif dloss == "tiny":
+        s["dloss"] *= 1e-25
+    elif dloss == "huge":
+        s["dloss"] *= 1e25
+    else:
+        for k in ("target", "index"):
+            if k in s:
+                s[k][:40] = -1
+        off[:40] = True
+        s["dloss"][off] = float("nan")
+    _hold(_call(s), s)
+
+
+def test_the_mean_loss_gradient_is_as_exact_as_its_rounding():
+    """With dloss = 1 / tokens for every token the error of the gradients' norm stays near that of
+    rounding them to bf16 (1.7e-3: 2^-7 / sqrt(12) of a value's power of two, the value anywhere
+    between two of them) and of rounding ds as well (sqrt(2) times that), wherever 1 / tokens lies
+    between two bf16 values."""
+    for count in (256, 271, 288, 300, 333, 383):
+        s = _inputs(512, 256, 2000, seed=22)
+        s["dloss"] = torch.full_like(s["dloss"], 1.0 / count)
+        got = _call(s)
+        ref, _ = reference(**s)
+        for k in ("dx", "dW"):
+            err = float((got[k].double() - ref[k]).norm() / ref[k].norm())
+            assert err < 2.0 ** -8 * 0.625, (count, k, err)
+
+
 @pytest.mark.parametrize("K", [0, 7])
 def test_several_pieces_of_the_vocabulary(K):
     """33000 tokens: 2048 vocabulary entries per piece at most, so three pieces of 4099."""
