@@ -719,9 +719,8 @@ class Mxfp:
 
     def _c(self) -> _Mxfp:
         r, c = self.rows, self.cols
-        return _Mxfp(_arr(self.codes, _U8, r * (c // 2), "codes"),
-                     _arr(self.scales, _U8, (r + 127) // 128 * ((c + 255) // 256) * 1024,
-                          "scales"), r, c)
+        return _Mxfp(_arr(self.codes, _U8, r * (c >> 1), "codes"),
+                     _arr(self.scales, _U8, (r + 127 >> 7) * (c + 255 >> 8) << 10, "scales"), r, c)
 
 
 def fq_mxfp_codes_bytes(rows: int, cols: int) -> int:

@@ -692,17 +692,21 @@ __device__ __forceinline__ void copy_row(const uint4* x, uint4* xc, int64_t row,
     xc[row * d8 + j] = has ? __ldcg(x + row * d8 + j) : make_uint4(0u, 0u, 0u, 0u);
 }
 
-// The reference dloss: that of the first token with a target, or 1 where there is none or it is
-// no ordinary number.  One block.
+// The reference dloss: that of the first token with a target among the first kLook, or 1 where
+// there is none or it is no ordinary number.  One block; `per` threads (a power of two up to 32)
+// ask about a token together.
+constexpr int kLook = 256;
+
 template <typename HasTarget>
-__device__ __forceinline__ void find_reference(int M, const float* dloss, float* gref,
+__device__ __forceinline__ void find_reference(int M, int per, const float* dloss, float* gref,
                                                HasTarget has) {
   __shared__ int first;
   if (threadIdx.x == 0) first = kNone;
   __syncthreads();
-  for (int base = 0; base < M; base += blockDim.x) {
-    const int i = base + static_cast<int>(threadIdx.x);
-    const bool hit = i < M && has(i);
+  const int at_once = static_cast<int>(blockDim.x) / per;
+  for (int base = 0; base < min(M, kLook); base += at_once) {
+    const int i = base + static_cast<int>(threadIdx.x) / per;
+    const bool hit = i < M && has(i, static_cast<int>(threadIdx.x) % per);
     if (hit) atomicMin(&first, i);
     if (__syncthreads_or(hit)) break;             // the block leaves as one
   }
@@ -771,12 +775,12 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   __syncthreads();
   if (threadIdx.x == 0) plogp[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
   if (xc && blockIdx.x == 0)
-    find_reference(M, dloss, gref, [&](int i) {
-      for (int k = 0; k < K; ++k)
-        if (entry_counts(__ldcg(index + static_cast<int64_t>(i) * K + k),
-                         __ldcg(logit + static_cast<int64_t>(i) * K + k), V))
-          return true;
-      return false;
+    find_reference(M, 32, dloss, gref, [&](int i, int j) {
+      const int64_t at = static_cast<int64_t>(i) * K;
+      bool any = false;
+      for (int k = j; k < K; k += 32)
+        any |= entry_counts(__ldcg(index + at + k), __ldcg(logit + at + k), V);
+      return any;
     });
 }
 
@@ -862,7 +866,7 @@ __global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int M, i
   const int32_t first = __ldcg(target + blockIdx.x);
   copy_row(x, xc, blockIdx.x, d8, first >= 0 && first < V);
   if (blockIdx.x == 0)
-    find_reference(M, dloss, gref, [&](int i) {
+    find_reference(M, 1, dloss, gref, [&](int i, int) {
       const int32_t t = __ldcg(target + i);
       return t >= 0 && t < V;
     });
@@ -1027,9 +1031,9 @@ fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStrea
 // pairs): as narrow as still does.  Else the width whose rounds take the least time, where a
 // round goes as its width + 64 columns for up to 128 tokens (which stream W: 39654 x 2440 for 16
 // tokens 51 us at 256 columns and two rounds, 46 at 144 and two, 51 at 128 and three) and + 256
-// for up to 512 (256 tokens, 32000 x 4096: 27.3 us a round at 256 columns, 18.9 at 128).  More
-// tokens have so many tiles that the widest are best (2048 tokens: 285 us at 256, 288 at 224).
-constexpr int kMinBn = 64;                      // where there are several rounds
+// for more (2048 tokens, 32000 x 4096: 20.3 us a round at 256 columns, 15.7 at 128).
+constexpr int kMinBn = 64;                      // where there are several rounds: few tokens,
+constexpr int kMinBnMany = 128;                 // and more than two row tiles
 
 int pick_bn(int R, int N, int sms) {
   const int cg = group_for(R), unit = 16 * cg;
@@ -1038,7 +1042,7 @@ int pick_bn(int R, int N, int sms) {
   int64_t least = -1;
   for (int bn = kBN; bn >= unit; bn -= unit) {
     const int64_t rounds = ceil_div(RT * ceil_div(N, bn), room);
-    if (rounds > 1 && bn < (RT <= 2 ? kMinBn : kBN)) break;
+    if (rounds > 1 && bn < (RT <= 2 ? kMinBn : kMinBnMany)) break;
     const int64_t cost = rounds * (bn + (cg == 1 ? 64 : 256));
     if (least < 0 || cost < least) least = cost, best = bn;
   }
@@ -1049,7 +1053,8 @@ int pick_bn(int R, int N, int sms) {
 int64_t most_tiles(int R, int N) {
   const int cg = group_for(R);
   const int64_t RT = ceil_div(R, kBM * cg);
-  return std::max<int64_t>(ceil_div(N, RT <= 2 ? kMinBn : kBN), kMaxSms / cg / RT);
+  return std::max<int64_t>(ceil_div(N, RT <= 2 ? kMinBn : kMinBnMany),
+                           kMaxSms / cg / RT);
 }
 
 // The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
