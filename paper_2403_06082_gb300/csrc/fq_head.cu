@@ -718,7 +718,8 @@ __device__ __forceinline__ void find_reference(int M, int per, const float* dlos
 
 // One block per token: the teacher's probabilities of its entries, in ascending order of the
 // vocabulary entry (rank of each entry by counting, K <= 1024), entries that do not count last;
-// and sum_k p_k log p_k.  For the gradient (xc) also the copy of x, and the reference dloss.
+// and sum_k p_k log p_k.  For the gradients also the copy of x (xc, where dW is wanted), and the
+// reference dloss (gref).
 constexpr int kSortThreads = 128;
 
 __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
@@ -774,7 +775,7 @@ __global__ void __launch_bounds__(kSortThreads) head_entries_kernel(
   if (lane == 0) red[warp] = h;
   __syncthreads();
   if (threadIdx.x == 0) plogp[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
-  if (xc && blockIdx.x == 0)
+  if (gref && blockIdx.x == 0)
     find_reference(M, 32, dloss, gref, [&](int i, int j) {
       const int64_t at = static_cast<int64_t>(i) * K;
       bool any = false;
@@ -854,8 +855,8 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(
   }
 }
 
-// The copy of x and the reference dloss where the target is all there is to prepare (cross
-// entropy).  One block per token.
+// The copy of x (xc, where dW is wanted: a block per token; else one block) and the reference
+// dloss, where the target is all there is to prepare (cross entropy).
 __global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int M, int d8,
                                                         const int32_t* target, int V, uint4* xc,
                                                         const float* dloss, float* gref,
@@ -863,8 +864,10 @@ __global__ void __launch_bounds__(256) head_copy_kernel(const uint4* x, int M, i
   pdl_wait();
   pdl_launch_dependents();                        // as in head_entries_kernel
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0;
-  const int32_t first = __ldcg(target + blockIdx.x);
-  copy_row(x, xc, blockIdx.x, d8, first >= 0 && first < V);
+  if (xc) {
+    const int32_t first = __ldcg(target + blockIdx.x);
+    copy_row(x, xc, blockIdx.x, d8, first >= 0 && first < V);
+  }
   if (blockIdx.x == 0)
     find_reference(M, 1, dloss, gref, [&](int i, int) {
       const int32_t t = __ldcg(target + i);
@@ -1169,8 +1172,8 @@ fq_status check_common(const void* x, int M, int d, const void* W, int V, const 
   return FQ_OK;
 }
 
-// The token's entries in ascending order: the target itself, or the sorted teacher's list; with xc,
-// the copy of x.
+// The token's entries in ascending order: the target itself, or the sorted teacher's list; with
+// dloss the reference, with xc the copy of x.
 fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, const void* x, int d,
                          void* xc, const float* dloss, const int32_t*& entry, const float*& prob, const float*& plogp,
                          cudaStream_t s) {
@@ -1182,8 +1185,9 @@ fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, c
   if (!t.logit) {
     entry = t.given;
     prob = plogp = nullptr;
-    if (xc)
-      e = launch(head_copy_kernel, M, 256, 0, s, x4, M, d / 8, t.given, V, xc4, dloss, gref, status);
+    if (dloss)
+      e = launch(head_copy_kernel, xc ? M : 1, 256, 0, s, x4, M, d / 8, t.given, V, xc4, dloss,
+                 gref, status);
   } else {
     auto* en = reinterpret_cast<int32_t*>(ws + L.entry);
     auto* pr = reinterpret_cast<float*>(ws + L.prob);
@@ -1192,7 +1196,7 @@ fq_status launch_entries(const Target& t, int M, int V, const Ws& L, char* ws, c
     prob = pr;
     plogp = pl;
     e = launch(head_entries_kernel, M, kSortThreads, 0, s, t.given, t.logit, t.K, V, 1.f / t.tau,
-               en, pr, pl, M, x4, d / 8, xc4, dloss, gref, status);
+               en, pr, pl, M, x4, d / 8, xc4, dloss, dloss ? gref : nullptr, status);
   }
   return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
@@ -1256,7 +1260,8 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
 
   const int32_t* entry = nullptr;
   const float *prob = nullptr, *plogp = nullptr;
-  if (const fq_status st = launch_entries(t, M, V, L, ws, x, d, xc, dloss, entry, prob, plogp, s))
+  if (const fq_status st = launch_entries(t, M, V, L, ws, x, d, dW ? xc : nullptr, dloss, entry,
+                                          prob, plogp, s))
     return st;
 
   const int P = piece_width(M, V);
@@ -1275,7 +1280,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
     {
       GemmArgs g{};
       GemmMaps m{};
-      if (!plan_logits(g, m, xc, Wq, M, Vc, d, sms, kDl) ||
+      if (!plan_logits(g, m, x, Wq, M, Vc, d, sms, kDl) ||
           !make_tmap(&m.out, ds, M, Vc, ldds, 32))
         return FQ_ERR_CUDA;
       g.status = status;
@@ -1290,7 +1295,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
       g.gref = reinterpret_cast<const float*>(ws + L.gref);
       g.ds = ds;
       g.ldds = ldds;
-      g.early_b = 1;
+      g.early_a = g.early_b = 1;
       if (const fq_status st = launch_logits<kDl>(m, g, sms, s)) return st;
     }
     GemmArgs g{};
