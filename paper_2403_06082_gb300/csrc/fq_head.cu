@@ -328,6 +328,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         pdl_wait();
         waited = true;
       }
+      // The logits' column tiles begin at places spread over k: if all began at 0, all would read
+      // the same lines of x at the same time (154 tokens, 7039 x 5976: 40 us so, 36 this way).
+      int kc = MODE == kGrad ? u.k0
+                             : static_cast<int>(static_cast<int64_t>(u.col / p.bn) * p.KB / p.NT);
       for (int kb = u.k0; kb < u.k1; ++kb, ++it) {
         ok = mbar_wait_warp(&empty[stage], phase ^ 1, abort_flag);
         if (!ok) break;
@@ -341,13 +345,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           // beyond the last one arrive as zeros)
           const int boxes = MODE == kGrad ? (mn ? 2 : 1) : p.per;
           const int block = MODE == kGrad ? kAtomBytes : (is_a ? p.a_block : p.b_block);
-          const int k = kb * kBK * (MODE == kGrad ? 1 : p.per);
+          const int k = kc * kBK * (MODE == kGrad ? 1 : p.per);
           for (int h = 0; h < boxes; ++h) {
             const int x = mn ? row + 64 * h : k + kBK * h, y = mn ? k : row;
             if (CG == 2) tma_load_2d_pair(dst + h * block, tm, bar, x, y, pol);
             else tma_load_2d(dst + h * block, tm, &full[stage], x, y, pol);
           }
         }
+        if (++kc == p.KB && MODE != kGrad) kc = 0;
         if (++stage == p.stages) stage = 0, phase ^= 1;
       }
     }
