@@ -233,7 +233,8 @@ __device__ __forceinline__ void bulk_wait() {
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-// A token's ascending entry list, walked along with the columns of a tile.
+// A token's ascending entry list, walked along with the columns of a tile.  Read through L1: the
+// next entries lie beside the last.
 struct EntryWalk {
   const int32_t* e;
   int k, E, next;
@@ -241,15 +242,15 @@ struct EntryWalk {
     int lo = 0, hi = E_;
     while (lo < hi) {                            // first entry >= from
       const int mid = (lo + hi) >> 1;
-      if (__ldcg(e + mid) < from) lo = mid + 1;
+      if (e[mid] < from) lo = mid + 1;
       else hi = mid;
     }
     k = lo;
-    next = k < E ? __ldcg(e + k) : kNone;
+    next = k < E ? e[k] : kNone;
   }
   __device__ __forceinline__ void step() {
     ++k;
-    next = k < E ? __ldcg(e + k) : kNone;
+    next = k < E ? e[k] : kNone;
   }
 };
 
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int q = 0; q < kChunk; ++q) v[q] = ex2(fmaf(v[q], c2, -lse2));
             while (w.next < p.v0 + n0 + c + cc + kChunk) {
               const int j = w.next - (p.v0 + n0 + c + cc);
-              const float pk = p.prob ? __ldcg(p.prob + lrow * p.E + w.k) : 1.f;
+              const float pk = p.prob ? p.prob[lrow * p.E + w.k] : 1.f;
 #pragma unroll
               for (int q = 0; q < kChunk; ++q) v[q] -= q == j ? pk : 0.f;
               w.step();
