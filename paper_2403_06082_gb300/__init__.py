@@ -643,20 +643,24 @@ _BF, _F32, _I32, _U8 = "bfloat16", "float32", "int32", "uint8"
 _dtypes = {}
 
 
+def _dtype(name: str):
+    import torch
+    _dtypes[name] = getattr(torch, name)
+    return _dtypes[name]
+
+
 def _arr(t, dtype: str, count: int, what: str):
     """_ptr of a tensor that has to hold at least `count` values of the named torch dtype (None
     passes through); what the C side cannot see is refused here."""
     if t is None:
         return None
-    want = _dtypes.get(dtype)
-    if want is None:
-        import torch
-        want = _dtypes[dtype] = getattr(torch, dtype)
-    if t.dtype is not want:
-        raise TypeError(f"{what}: {want} expected, got {t.dtype}")
+    if t.dtype is not (_dtypes.get(dtype) or _dtype(dtype)):
+        raise TypeError(f"{what}: torch.{dtype} expected, got {t.dtype}")
     if t.numel() < count:
         raise ValueError(f"{what}: {count} values expected, got {t.numel()}")
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError("libframequant takes contiguous row-major tensors only")
+    return t.data_ptr()
 
 
 def fq_head_workspace_bytes(M: int, d: int, V: int, K: int = 1) -> int:
