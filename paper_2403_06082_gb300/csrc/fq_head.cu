@@ -1103,24 +1103,34 @@ bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, 
   return make_tmap(&m.a, x, R, d, d, g.a_rows) && make_tmap(&m.b, W, N, d, d, g.bn / cg);
 }
 
-constexpr int64_t kPieceBytes = 128ll << 20;    // ds of one piece of the vocabulary
+// ds of one piece of the vocabulary, at most.  With dW half of what dx alone gets: ds then stays in
+// L2 between the launch that writes it and the one that reads it twice, and dW's tiles even out the
+// rounds of dx (4096 tokens, 32000 x 4096: 1563 us at 64 MiB, 1631 at 128).  dx alone pays for every
+// piece with another pass over its fp32 slots (1099 us at 128 MiB, 1133 at 64).
+constexpr int64_t kPieceBytes = 128ll << 20;
+constexpr int64_t kPieceBytesBoth = 64ll << 20;
 constexpr int kMinPiece = 2048;
 constexpr int kMaxSlots = 32;                   // fp32 slots of a dx split over the vocabulary
 
-// Vocabulary entries per piece: as many as kPieceBytes of ds hold (at least kMinPiece), in
-// pieces of equal size rounded up to 256.
-int piece_width(int M, int V) {
-  const int64_t most = std::max<int64_t>(kMinPiece, kPieceBytes / 2 / M);
+// Vocabulary entries per piece: as many as the bytes of ds hold (at least kMinPiece), in pieces of
+// equal size rounded up to 256.
+int piece_width(int M, int V, bool both) {
+  const int64_t most =
+      std::max<int64_t>(kMinPiece, (both ? kPieceBytesBoth : kPieceBytes) / 2 / M);
   const int64_t n = ceil_div(V, most);
   return static_cast<int>(std::min<int64_t>(round_up(V, 256), round_up(ceil_div(V, n), 256)));
 }
 
-// Most ways the contraction of dx over a piece is split: where its tiles are fewer than the pairs.
+// Most ways the contraction of dx over a piece is split: where its tiles are fewer than the pairs,
+// and their slots take no more than kSlotBytes.
+constexpr int64_t kSlotBytes = 128ll << 20;
+
 int most_splits(int M, int d, int Vc, int sms) {
   const int64_t tiles = ceil_div(M, 2 * kBM) * ceil_div(d, kBN);
   if (tiles >= std::min(sms, kMaxSms) / 2) return 1;
   return static_cast<int>(std::max<int64_t>(
-      1, std::min<int64_t>(kMaxSlots, ceil_div(Vc, kBK) / 8)));
+      1, std::min<int64_t>({kMaxSlots, ceil_div(Vc, kBK) / 8,
+                            kSlotBytes / 4 / M / d})));
 }
 
 struct Ws {
@@ -1144,13 +1154,14 @@ Ws ws_layout(int M, int d, int V, int K, bool grad) {
     L.zt = take(mk);
     L.part = take(static_cast<size_t>(most_tiles(M, V)) * 2 * M * 8);
   } else {
-    const int P = piece_width(M, V);
+    // for dx alone, dW alone or both; sized for any SM count
+    const int P = piece_width(M, V, false), P2 = piece_width(M, V, true);
     L.xc = take(static_cast<size_t>(M) * d * 2);
     // the pitch leaves room for the last tile's columns beyond the piece
     L.ds = take(static_cast<size_t>(M) * (P + kBN) * 2);
-    // sized for any SM count
-    const int S = most_splits(M, d, std::min(P, V), kMaxSms);
-    L.slots = take(S > 1 || P < V ? static_cast<size_t>(S) * M * d * 4 : 0);
+    const int S = std::max(most_splits(M, d, std::min(P, V), kMaxSms),
+                           most_splits(M, d, std::min(P2, V), kMaxSms));
+    L.slots = take(S > 1 || P2 < V ? static_cast<size_t>(S) * M * d * 4 : 0);
   }
   L.total = off;
   return L;
@@ -1270,7 +1281,7 @@ fq_status head_grad(const void* x, int M, int d, const void* W, int V, const Tar
                                           prob, plogp, s))
     return st;
 
-  const int P = piece_width(M, V);
+  const int P = piece_width(M, V, dW != nullptr);
   const int pieces = static_cast<int>(ceil_div(V, P));
   const int64_t ldds = P + kBN;
   const int most = most_splits(M, d, std::min(P, V), sms);

@@ -67,7 +67,7 @@ static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 constexpr int kNumBars = 2 * kMaxStages + 5;
 constexpr int kFuseTokens = 16;
 constexpr int kFuseStages = 32;                 // FUSE: k range of a CTA, in stages
-constexpr int kFuseValues = 16 * 1024;          // FUSE: tokens x k range of a CTA
+constexpr int kFuseValues = 8 * 1024;           // FUSE: tokens x k range of a CTA
 constexpr int kXBlock = kFuseTokens * kKStage / 2;            // FUSE: x's codes of a stage
 constexpr int kXScales = kFuseTokens * kKStage / 32;          // FUSE: and their scales
 constexpr int kTailBytes = kNumBars * 8 + 16;
