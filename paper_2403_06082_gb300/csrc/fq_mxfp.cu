@@ -30,8 +30,9 @@
 //
 // Up to 16 tokens the product takes bf16 x itself (FUSE): each CTA's epilogue warps quantise its k
 // range of x into shared memory, for all of its tiles, while W's first stages arrive.  One launch
-// instead of two; the range is bounded by kFuseStages and kFuseValues, beyond which every CTA
-// quantising the same x costs more than a kernel that does it once.
+// instead of two: 8 tokens, 4096 x 4096 6.5 us, not 7.9.  Beyond kFuseValues every CTA quantising
+// the same x costs more than a kernel that does it once: 4 tokens, 11008 x 4096 (16384 values)
+// 9.3 us fused and 8.4 in two launches, 16 tokens 14.2 and 8.4.
 //
 // Warp roles: warp 0 producer of W's codes, warp 1 TMEM owner + MMA issuer (of the first CTA of a
 // pair), warps 2-9 epilogue (thread = accumulator row, half of the tokens), warps 10-17 scales,
@@ -65,8 +66,8 @@ constexpr int kAhead = 2;                       // of its stages that a group of
 static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 
 constexpr int kNumBars = 2 * kMaxStages + 5;
+constexpr int kMaxSplit = 8;                    // SPLIT: CTAs on one tile, at most
 constexpr int kFuseTokens = 16;
-constexpr int kFuseStages = 32;                 // FUSE: k range of a CTA, in stages
 constexpr int kFuseValues = 8 * 1024;           // FUSE: tokens x k range of a CTA
 constexpr int kXBlock = kFuseTokens * kKStage / 2;            // FUSE: x's codes of a stage
 constexpr int kXScales = kFuseTokens * kKStage / 32;          // FUSE: and their scales
@@ -148,9 +149,12 @@ __device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t adesc, uint6
   }
 }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr)
+               : "memory");
   return v;
 }
 
@@ -557,18 +561,34 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (CG == 2) cluster_sync();
   if (SPLIT) {
     cluster_sync();
-    // token c of the tile is finished by rank c mod KS: parts added in rank order
+    // token c of the tile is finished by rank c mod KS, four rows a thread: parts added in rank order
     const int n0 = tile_n0(first), row0 = tile_rg(first) * kBM;
     const int tokens = min(p.bn, p.M - n0);
     const uint32_t mine = smem_u32(smem);
+    const bool whole = p.R % 4 == 0;
     if (!*abort_flag) {
-      for (int i = threadIdx.x; i < kBM * ((tokens - rank + p.KS - 1) / p.KS); i += kThreads) {
-        const int r = i % kBM, c = i / kBM * p.KS + rank;
+      const int r = (threadIdx.x & 31) * 4;
+      for (int c = (threadIdx.x >> 5) * p.KS + rank; c < tokens; c += kThreads / 32 * p.KS) {
         const uint32_t at = mine + static_cast<uint32_t>(c * kBM + r) * 4;
-        float s = 0.f;
-        for (int q = 0; q < p.KS; ++q) s += ld_cluster_f32(mapa(at, static_cast<uint32_t>(q)));
-        if (row0 + r < p.R)
-          p.y[static_cast<int64_t>(n0 + c) * p.R + row0 + r] = __float2bfloat16_rn(s);
+        float4 part[kMaxSplit];
+#pragma unroll
+        for (int q = 0; q < kMaxSplit; ++q)
+          if (q < p.KS) part[q] = ld_cluster_f32x4(mapa(at, static_cast<uint32_t>(q)));
+        float4 s = part[0];
+#pragma unroll
+        for (int q = 1; q < kMaxSplit; ++q)
+          if (q < p.KS) s.x += part[q].x, s.y += part[q].y, s.z += part[q].z, s.w += part[q].w;
+        __nv_bfloat16* dst = p.y + static_cast<int64_t>(n0 + c) * p.R + row0 + r;
+        __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+        if (whole && row0 + r < p.R) {
+          *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<uint32_t*>(&lo),
+                                                      *reinterpret_cast<uint32_t*>(&hi));
+        } else {
+          const __nv_bfloat16 v[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (row0 + r + q < p.R) dst[q] = v[q];
+        }
       }
     }
     cluster_sync();
@@ -750,11 +770,15 @@ fq_status quantize(const void* x, const fq_mxfp& q, cudaStream_t s) {
              : FQ_ERR_CUDA;
 }
 
-// CTAs (CG = 2: pairs) that the device runs at once.
+// fit[i]: clusters of 1 << i CTAs that the device runs at once (CTAs and pairs, or with SPLIT all).
+struct Room {
+  int fit[4];
+};
+
 template <int CG, bool SPLIT, bool FUSE>
-fq_status prepare_product(int sms, int& room) {
+fq_status prepare_product(int sms, Room& room) {
   static std::mutex mu;
-  static std::map<int, int> fit;
+  static std::map<int, Room> fit;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return FQ_ERR_CUDA;
   std::lock_guard<std::mutex> lock(mu);
@@ -764,15 +788,17 @@ fq_status prepare_product(int sms, int& room) {
                              cudaFuncAttributeMaxDynamicSharedMemorySize,
                              kSmemMost) != cudaSuccess)
       return FQ_ERR_CUDA;
-    int n = sms;
-    if (CG == 2) {
+    Room r{{sms, 0, 0, 0}};
+    for (int i = 1; i < 4; ++i) {
+      const int size = 1 << i;
+      if (SPLIT ? size > kMaxSplit : size != CG) continue;
       cudaLaunchConfig_t cfg{};
-      cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2));
+      cfg.gridDim = dim3(static_cast<unsigned>(sms / size * size));
       cfg.blockDim = dim3(kThreads);
       cfg.dynamicSmemBytes = kSmemMost;
       cudaLaunchAttribute attr[1];
       attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = 2;
+      attr[0].val.clusterDim.x = static_cast<unsigned>(size);
       attr[0].val.clusterDim.y = 1;
       attr[0].val.clusterDim.z = 1;
       cfg.attrs = attr;
@@ -782,9 +808,9 @@ fq_status prepare_product(int sms, int& room) {
               cudaSuccess ||
           most < 1)
         return FQ_ERR_CUDA;
-      n = std::min(sms / 2, most);
+      r.fit[i] = std::min(sms / size, most);
     }
-    it = fit.emplace(dev, n).first;
+    it = fit.emplace(dev, r).first;
   }
   room = it->second;
   return FQ_OK;
@@ -793,56 +819,79 @@ fq_status prepare_product(int sms, int& room) {
 template <int CG, bool SPLIT, bool FUSE>
 fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const ProdArgs& a, int sms,
                          cudaStream_t s) {
-  int room = 0;
+  Room room{};
   if (const fq_status st = prepare_product<CG, SPLIT, FUSE>(sms, room)) return st;
-  const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room) * CG;
+  const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room.fit[CG - 1]) * CG;
   return launch(mxfp_product_kernel<CG, SPLIT, FUSE>, dim3(static_cast<unsigned>(grid)), kThreads,
-                static_cast<size_t>(a.stages) * a.stage_bytes + a.x_bytes + kTailBytes + 1024, SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
+                static_cast<size_t>(a.stages) * a.stage_bytes + a.x_bytes + kTailBytes + 1024,
+                SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
 }
 
-// Tokens per tile: all of up to 192 in one tile.  More go by tiles of 128 or 192, whose first
-// token is a multiple of 64 (scales of X then start on an even column of their tile), whichever
-// takes less time: a stage took 303 ns at 128 tokens and 344 at 192 (d = 8192, pairs), so time
-// goes as the rounds of tiles over the SMs x (tokens + 345).
-int pick_bn(int M, int R, int sms) {
-  if (M <= kBN) return static_cast<int>(round_up(M, 16));
-  auto cost = [&](int bn) {
-    const int64_t pairs = ceil_div(R, 2 * kBM) * ceil_div(M, bn);
-    const int64_t rounds = pairs >= sms / 2 ? ceil_div(pairs, sms / 2)
-                                            : ceil_div(ceil_div(R, kBM) * ceil_div(M, bn), sms);
-    return rounds * (bn + 345);
-  };
-  return cost(128) < cost(192) ? 128 : 192;
+// The tiles of M tokens and W.  Of every width (all of up to 192 tokens, or tiles of 64, 128 or 192,
+// as scales of X have to start on an even column of their tile), by one CTA, a pair, or 2 to 8 CTAs
+// that split k where all of them fit at once, the one that takes the least time.  In ns, fitted to 4 to 43 stages of
+// 1024 to 28672 rows:
+//   a stage 210 up to 128 tokens, 250 at 192; one of several rounds of tiles its stages, or 500 + 7
+//   a token if storing the tile before takes longer, and 15% more on single CTAs (their reads from
+//   L2: 4096 tokens, 28672 x 8192 260 us in pairs, 314 without); the last tile 7 a token; a split
+//   1500 + 8 a token for the exchange.
+// Measured, with what a rule of all tokens to a tile and as many splits as fit took: 256 tokens,
+// 4096 x 4096 6.7 us (64 wide, no split) and 11.0; 128 tokens, 1024 x 4096 6.3 (64 wide, 4 splits)
+// and 7.6 (128 wide, 8); 192 tokens, 4096 x 1024 3.9 (64 wide) and 7.8 (192 wide, 2 splits).
+// A split pays at one token: 1024 x 11008 5.6 us with 8, 11.8 without; 4096 x 4096 5.4 with 4, 6.4;
+// 4096 x 1024 4.8 with 2, 3.7 without.
+void plan_tiles(ProdArgs& a, int& cg, int sms, const Room& pairs, const Room& splits) {
+  const int most = a.M <= kBN ? static_cast<int>(round_up(a.M, 16)) : kBN;
+  int64_t least = -1;
+  for (const int bn : {most, 64, 128}) {
+    if (bn > most) continue;                      // (up to 16 tokens: 16, what FUSE has room for)
+    const int64_t TT = ceil_div(a.M, bn);
+    for (int c = 1; c <= 2; ++c) {
+      const int64_t units = ceil_div(a.R, c * kBM) * TT;
+      const int64_t rounds = ceil_div(units, c == 2 ? pairs.fit[1] : sms);
+      const int64_t stage = 210 + std::max(0, bn - 128) * 5 / 8;
+      for (int i = 0; i < (c == 1 ? 4 : 1); ++i) {
+        if (i && (units > splits.fit[i] || a.KB < 2 << i)) break;
+        int64_t round = ceil_div(a.KB, 1 << i) * stage;
+        if (rounds > 1) round = std::max<int64_t>(round, 500 + 7 * bn) * (c == 1 ? 115 : 100) / 100;
+        const int64_t time = rounds * round + 7 * bn + (i ? 1500 + 8 * bn : 0);
+        if (least < 0 || time < least) {
+          least = time;
+          a.bn = bn;
+          a.KS = 1 << i;
+          cg = c;
+        }
+      }
+    }
+  }
 }
 
-// The tiles of M tokens and W, and the split of k.
-ProdArgs plan_product(int M, const fq_mxfp& W, int sms, int& cg) {
-  ProdArgs a{};
+fq_status plan_product(ProdArgs& a, int M, const fq_mxfp& W, int sms, int& cg) {
+  Room pairs{}, splits{};
+  if (const fq_status st = prepare_product<2, false, false>(sms, pairs)) return st;
+  if (const fq_status st = prepare_product<1, true, false>(sms, splits)) return st;
   a.R = W.rows;
   a.M = M;
   a.K = W.cols;
-  a.bn = pick_bn(a.M, a.R, sms);
-  a.TT = static_cast<int>(ceil_div(a.M, a.bn));
-  // pairs of CTAs once their tiles fill the SMs
-  cg = ceil_div(a.R, 2 * kBM) * a.TT >= sms / 2 ? 2 : 1;
-  a.RT = static_cast<int>(ceil_div(a.R, cg * kBM));
   a.KB = stages_of(W.cols);
+  plan_tiles(a, cg, sms, pairs, splits);
+  a.TT = static_cast<int>(ceil_div(a.M, a.bn));
+  a.RT = static_cast<int>(ceil_div(a.R, cg * kBM));
   a.units = a.RT * a.TT;
-  a.KS = 1;
-  while (cg == 1 && a.KS < 8 && a.units * a.KS * 2 <= sms && a.KB >= a.KS * 4) a.KS *= 2;
   a.kbs = static_cast<int>(ceil_div(a.KB, a.KS));
   a.sw = W.scales;
   a.wgroups = static_cast<int>(ceil_div(a.R, 128));
   a.xgroups = static_cast<int>(ceil_div(a.M, 128));
-  return a;
+  return FQ_OK;
 }
 
 fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, int sms,
                   bool early_w, cudaStream_t s) {
   int cg = 1;
-  ProdArgs a = plan_product(X.rows, W, sms, cg);
+  ProdArgs a{};
+  if (const fq_status st = plan_product(a, X.rows, W, sms, cg)) return st;
   a.stage_bytes = stage_bytes(a.bn / cg);
   a.stages = stages_for(a.stage_bytes, 0);
   a.sx = X.scales;
@@ -863,9 +912,10 @@ bool fused_product(const void* x, int M, const fq_mxfp& W, void* y, int32_t* sta
                    cudaStream_t s, fq_status& st) {
   if (M > kFuseTokens) return false;
   int cg = 1;
-  ProdArgs a = plan_product(M, W, sms, cg);
+  ProdArgs a{};
+  if ((st = plan_product(a, M, W, sms, cg)) != FQ_OK) return true;
   const int range = a.KS > 1 ? a.kbs : a.KB;
-  if (range > kFuseStages || M * range * kKStage > kFuseValues) return false;
+  if (M * range * kKStage > kFuseValues) return false;
   if (cg == 2) {                                  // tiles of one CTA: W is what is read
     a.RT = static_cast<int>(ceil_div(a.R, kBM));
     a.units = a.RT * a.TT;
