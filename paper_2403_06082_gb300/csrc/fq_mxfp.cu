@@ -558,6 +558,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   tc_fence_before_sync();
   __syncthreads();
+  __syncwarp();
   if (CG == 2) cluster_sync();
   if (SPLIT) {
     cluster_sync();
@@ -591,6 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
+    __syncwarp();                                 // the cluster's barrier takes whole warps
     cluster_sync();
   }
   if (warp == 1) {

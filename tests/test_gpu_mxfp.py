@@ -123,6 +123,20 @@ def test_linear_of_few_tokens(M, d, V):
         assert ((y.double() - ref).abs() <= _bound(X, W, ref)).all()
 
 
+@pytest.mark.parametrize("M,d,V", [
+    (256, 4096, 1031), (129, 4096, 520), (100, 11008, 1024), (192, 1024, 4096), (64, 4096, 4093),
+    (97, 5472, 300), (40, 8192, 1000), (320, 288, 8805), (1275, 288, 2221), (700, 2048, 5504)])
+def test_linear_of_every_kind_of_tile(M, d, V):
+    """Tiles of 64, 128 and 192 tokens, one tile of all of them; one CTA, pairs, 2 to 8 CTAs that
+    split k, with a last part that is shorter; rows of y that are not a multiple of 4."""
+    x, w = _matrix(M, d, 13), _matrix(V, d, 14, loud=False)
+    X, W = dequantised(x).to(DEV), dequantised(w).to(DEV)
+    ref = X @ W.T
+    y = _linear(x, w).double()
+    over = (y - ref).abs() - _bound(X, W, ref)
+    assert (over <= 0).all(), (float(over.max()), int(over.argmax()))
+
+
 @pytest.mark.parametrize("M", [3, 300])
 def test_product_of_two_quantised_is_the_linear(M):
     x, w = _matrix(M, 1024, 3), _matrix(500, 1024, 4, loud=False)
