@@ -25,7 +25,7 @@
 // With CG = 2 a cluster of two CTAs works on one tile of 256 x bn: each CTA stages its 128 rows
 // of A and half of the rows of B, one MMA reads both CTAs' shared memory, and each CTA finishes
 // its own 128 rows.  Against one CTA per 128 x 256 tile this halves the reads of B per SM.
-// Results of at most 128 rows take CG = 1.
+// Up to 128 tokens, and where pairs would waste too many rows, logits take CG = 1.
 //
 // kLse adds the accumulator up in registers every kSegBlocks k-blocks.  The tensor core cuts off
 // what is below its accumulator's last bit at every step, so a long sum drifts towards zero: at
@@ -85,6 +85,7 @@ struct GemmMaps {
 
 struct GemmArgs {
   int R, N;                   // rows of A, rows of B (columns of the result); kGrad: of dx
+  int cg;                     // CTAs per tile (the host chooses the kernel by it)
   int bn;                     // columns per tile (multiple of 16 CG; kGrad: kBN)
   int RT, NT, KB, KS, kbs, units;
   int R2, RT2, KB2, units2;   // kGrad: the same of dW (columns as dx, no split)
@@ -666,6 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // before the TMEM goes and the pair parts.
   tc_fence_before_sync();
   __syncthreads();
+  __syncwarp();
   if (CG == 2) cluster_sync();
   if (warp == 1) {
     tc_fence_after_sync();
@@ -1027,13 +1029,22 @@ fq_status launch_gemm_cg(const GemmMaps& m, const GemmArgs& g, int sms, cudaStre
                                                                                    : FQ_ERR_CUDA;
 }
 
-// CTAs per tile of the logit products: a pair where there are more than one CTA's tokens.
-int group_for(int R) { return R > kBM ? 2 : 1; }
+// CTAs per tile of the logit products.  More tokens than one CTA's rows take pairs, which read half
+// as much from L2: 2000 tokens, 32000 x 4096 276 us, 311 on single CTAs; 512, 10000 x 2048 26.3 and
+// 27.1; 256, 32000 x 4096 54.0 and 64.3.  Three row tiles of single CTAs waste less than two of
+// pairs, which pays until L2 is the bound: 300 tokens, 10000 x 4096 31.2 us and 39.7 in pairs,
+// 32000 x 1024 27.2 and 30.5, 32000 x 4096 81.6 and 81.2, 276 tokens, 53805 x 5768 273 and 247.
+constexpr int64_t kSinglesValues = 96ll << 20;  // of W
+
+int group_for(int R, int N, int d) {
+  const bool singles = ceil_div(R, kBM) == 3 && static_cast<int64_t>(N) * d <= kSinglesValues;
+  return R <= kBM || singles ? 1 : 2;
+}
 
 template <int MODE>
 fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStream_t s) {
-  return group_for(g.R) == 2 ? launch_gemm_cg<MODE, 2>(m, g, sms, s)
-                             : launch_gemm_cg<MODE, 1>(m, g, sms, s);
+  return g.cg == 2 ? launch_gemm_cg<MODE, 2>(m, g, sms, s)
+                   : launch_gemm_cg<MODE, 1>(m, g, sms, s);
 }
 
 // Columns per tile of the logit products, a multiple of 16 CG.  All tiles at once on the SMs (or
@@ -1044,8 +1055,8 @@ fq_status launch_logits(const GemmMaps& m, const GemmArgs& g, int sms, cudaStrea
 constexpr int kMinBn = 64;                      // where there are several rounds: few tokens,
 constexpr int kMinBnMany = 128;                 // and more than two row tiles
 
-int pick_bn(int R, int N, int sms) {
-  const int cg = group_for(R), unit = 16 * cg;
+int pick_bn(int R, int N, int cg, int sms) {
+  const int unit = 16 * cg;
   const int64_t RT = ceil_div(R, kBM * cg), room = std::min(sms, kMaxSms) / cg;
   int best = kBN;
   int64_t least = -1;
@@ -1058,12 +1069,14 @@ int pick_bn(int R, int N, int sms) {
   return best;
 }
 
-// Most column tiles of the logit products on any device.
+// Most column tiles of the logit products on any device, by single CTAs or pairs.
 int64_t most_tiles(int R, int N) {
-  const int cg = group_for(R);
-  const int64_t RT = ceil_div(R, kBM * cg);
-  return std::max<int64_t>(ceil_div(N, RT <= 2 ? kMinBn : kMinBnMany),
-                           kMaxSms / cg / RT);
+  int64_t most = 1;
+  for (int cg = 1; cg <= 2; ++cg) {
+    const int64_t RT = ceil_div(R, kBM * cg);
+    most = std::max({most, ceil_div(N, RT <= 2 ? kMinBn : kMinBnMany), kMaxSms / cg / RT});
+  }
+  return most;
 }
 
 // The ring of operand stages, a_bytes and b_bytes to a k block.  A stage costs its roles some 400
@@ -1086,10 +1099,10 @@ void plan_ring(GemmArgs& g, int mode, int a_bytes, int b_bytes) {
 // The tiles and operand maps of a logit product: R tokens x N vocabulary entries.
 bool plan_logits(GemmArgs& g, GemmMaps& m, const void* x, const void* W, int R, int N, int d,
                  int sms, int mode) {
-  const int cg = group_for(R);
+  const int cg = g.cg = group_for(R, N, d);
   g.R = R;
   g.N = N;
-  g.bn = pick_bn(R, N, sms);
+  g.bn = pick_bn(R, N, cg, sms);
   g.RT = static_cast<int>(ceil_div(R, kBM * cg));
   g.NT = static_cast<int>(ceil_div(N, g.bn));
   g.KB = g.kbs = static_cast<int>(ceil_div(d, kBK));

@@ -104,6 +104,13 @@ def test_cross_entropy_and_gradients(M, d, V):
     _hold(_call(s), s)
 
 
+@pytest.mark.parametrize("M,d,V", [(257, 1032, 130), (384, 1032, 2049), (300, 4096, 4099),
+                                   (385, 520, 4099), (300, 4096, 24577)])
+def test_three_row_tiles_by_single_ctas_and_by_pairs(M, d, V):
+    s = _inputs(M, d, V, seed=M + V)
+    _hold(_call(s), s)
+
+
 @pytest.mark.parametrize("K,tau", [(1, 1.0), (5, 2.0), (64, 1.5), (300, 4.0), (1024, 0.5)])
 @pytest.mark.parametrize("M,d,V", [(3, 72, 17), (130, 256, 1031), (300, 520, 4099)])
 def test_distillation_and_gradients(M, d, V, K, tau):
