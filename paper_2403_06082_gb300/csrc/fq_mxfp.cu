@@ -25,8 +25,11 @@
 // tiles' traffic from L2 is what bounds a large product, and this cuts it by 28%.
 //
 // Few tokens read W once at memory speed; the tiles are then too few for the SMs, so a cluster of
-// KS CTAs splits the k range of one tile and adds the parts up, in rank order, through
-// distributed shared memory.
+// KS CTAs splits the k range of one tile.  Each CTA finishes every KS-th token: all write their parts
+// of it to that CTA's shared memory, where they are added up in rank order.  (Parts kept at home and
+// read by their adder cost a second barrier: 64 tokens, 1024 x 4096 6.0 us, 4.7 this way; one token,
+// 4096 x 4096 5.4 and 5.2.)  The room for parts leaves five stages at 128 tokens, the most that a
+// split tile has.
 //
 // Up to 16 tokens the product takes bf16 x itself (FUSE): each CTA's epilogue warps quantise its k
 // range of x into shared memory, for all of its tiles, while W's first stages arrive.  One launch
@@ -66,7 +69,8 @@ constexpr int kAhead = 2;                       // of its stages that a group of
 static_assert(kSfCol + kSlots * kSfCols <= kTmemCols, "tensor memory");
 
 constexpr int kNumBars = 2 * kMaxStages + 5;
-constexpr int kMaxSplit = 8;                    // SPLIT: CTAs on one tile, at most
+constexpr int kMaxSplit = 8;                    // SPLIT: CTAs on one tile, at most (a power of two)
+constexpr int kSplitTokens = 128;               // SPLIT: tokens of a tile, at most
 constexpr int kFuseTokens = 16;
 constexpr int kFuseValues = 8 * 1024;           // FUSE: tokens x k range of a CTA
 constexpr int kXBlock = kFuseTokens * kKStage / 2;            // FUSE: x's codes of a stage
@@ -149,13 +153,8 @@ __device__ __forceinline__ void umma_mxf4(uint32_t tmem_d, uint64_t adesc, uint6
   }
 }
 
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(addr)
-               : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 // Two values to E2M1 codes: to nearest, ties to the even code, saturating; hi in bits 4-7.
@@ -201,7 +200,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* xcodes = smem + p.stages * p.stage_bytes;             // FUSE
-  uint64_t* full = reinterpret_cast<uint64_t*>(xcodes + (FUSE ? p.x_bytes : 0));
+  float* parts = reinterpret_cast<float*>(xcodes + (FUSE ? p.x_bytes : 0));   // SPLIT
+  uint64_t* full = reinterpret_cast<uint64_t*>(parts + (SPLIT ? p.bn * kBM : 0));
   // full: codes of both CTAs in shared memory, scales of both in TMEM (first CTA's barriers);
   // empty: they have been read
   uint64_t* empty = full + kMaxStages;
@@ -246,6 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before_sync();
   __syncthreads();
   if (CG == 2) cluster_sync();
+  if (SPLIT) cluster_arrive();                    // waited for before a write to another CTA
   tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
@@ -471,6 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r_in_tile = quarter * 32 + lane;
     const int hw = (p.bn / 2 + 15) / 16 * 16;
     const int h0 = half * hw, h1 = half ? p.bn : hw;
+    if (SPLIT) cluster_wait();
     pdl_wait();
     if (FUSE) {
       // codes as TMA would leave them: 16 rows of 128 bytes a stage under the 128-byte swizzle
@@ -529,10 +531,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int q = 0; q < 16; ++q) v[q] = 0.f;
         }
         if (SPLIT) {
-          // this rank's part, token major, over the stages: all of their copies and MMAs are done
-          float* part = reinterpret_cast<float*>(smem);
+          // token c is finished by rank c mod KS, which gets the parts of all ranks side by side
+          const uint32_t at = smem_u32(parts + rank * kBM + r_in_tile);
 #pragma unroll
-          for (int q = 0; q < 16; ++q) part[(c + q) * kBM + r_in_tile] = v[q];
+          for (int q = 0; q < 16; ++q) {
+            const uint32_t t = static_cast<uint32_t>(c + q), owner = t & (p.KS - 1u);
+            if (c + q < cols) st_cluster_f32(mapa(at + (t - owner) * kBM * 4, owner), v[q]);
+          }
         } else if (row < p.R) {
           // a warp's 32 rows are 64 contiguous bytes of a token; the address moves by additions (a
           // check and a product for each store made 3330 tokens of 8832 x 288 take 35 us, not 19)
@@ -556,44 +561,41 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
 
+  if (SPLIT && (warp < 2 || warp > 9)) {
+    __syncwarp();
+    cluster_wait();
+  }
   tc_fence_before_sync();
   __syncthreads();
-  __syncwarp();
-  if (CG == 2) cluster_sync();
-  if (SPLIT) {
-    cluster_sync();
-    // token c of the tile is finished by rank c mod KS, four rows a thread: parts added in rank order
-    const int n0 = tile_n0(first), row0 = tile_rg(first) * kBM;
-    const int tokens = min(p.bn, p.M - n0);
-    const uint32_t mine = smem_u32(smem);
-    const bool whole = p.R % 4 == 0;
-    if (!*abort_flag) {
-      const int r = (threadIdx.x & 31) * 4;
-      for (int c = (threadIdx.x >> 5) * p.KS + rank; c < tokens; c += kThreads / 32 * p.KS) {
-        const uint32_t at = mine + static_cast<uint32_t>(c * kBM + r) * 4;
-        float4 part[kMaxSplit];
-#pragma unroll
-        for (int q = 0; q < kMaxSplit; ++q)
-          if (q < p.KS) part[q] = ld_cluster_f32x4(mapa(at, static_cast<uint32_t>(q)));
-        float4 s = part[0];
-#pragma unroll
-        for (int q = 1; q < kMaxSplit; ++q)
-          if (q < p.KS) s.x += part[q].x, s.y += part[q].y, s.z += part[q].z, s.w += part[q].w;
-        __nv_bfloat16* dst = p.y + static_cast<int64_t>(n0 + c) * p.R + row0 + r;
-        __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
-        if (whole && row0 + r < p.R) {
-          *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<uint32_t*>(&lo),
-                                                      *reinterpret_cast<uint32_t*>(&hi));
-        } else {
-          const __nv_bfloat16 v[4] = {lo.x, lo.y, hi.x, hi.y};
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (row0 + r + q < p.R) dst[q] = v[q];
-        }
-      }
-    }
+  if (CG == 2 || SPLIT) {
     __syncwarp();                                 // the cluster's barrier takes whole warps
     cluster_sync();
+  }
+  if (SPLIT && !*abort_flag) {
+    // this rank's tokens, four rows a thread: parts added in rank order
+    const int n0 = tile_n0(first), row0 = tile_rg(first) * kBM;
+    const int tokens = min(p.bn, p.M - n0), r = lane * 4;
+    for (int c = warp * p.KS + rank; c < tokens; c += kThreads / 32 * p.KS) {
+      const float* at = parts + (c - rank) * kBM + r;
+      float4 s = *reinterpret_cast<const float4*>(at);
+#pragma unroll
+      for (int q = 1; q < kMaxSplit; ++q)
+        if (q < p.KS) {
+          const float4 v = *reinterpret_cast<const float4*>(at + q * kBM);
+          s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+        }
+      __nv_bfloat16* dst = p.y + static_cast<int64_t>(n0 + c) * p.R + row0 + r;
+      __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+      if (p.R % 4 == 0 && row0 + r < p.R) {
+        *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<uint32_t*>(&lo),
+                                                    *reinterpret_cast<uint32_t*>(&hi));
+      } else {
+        const __nv_bfloat16 v[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (row0 + r + q < p.R) dst[q] = v[q];
+      }
+    }
   }
   if (warp == 1) {
     tc_fence_after_sync();
@@ -772,6 +774,9 @@ fq_status quantize(const void* x, const fq_mxfp& q, cudaStream_t s) {
              : FQ_ERR_CUDA;
 }
 
+// Shared memory of a split tile's parts, as many as the tile has values.
+int part_bytes(const ProdArgs& a) { return a.KS > 1 ? a.bn * kBM * 4 : 0; }
+
 // fit[i]: clusters of 1 << i CTAs that the device runs at once (CTAs and pairs, or with SPLIT all).
 struct Room {
   int fit[4];
@@ -825,7 +830,8 @@ fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const Pro
   if (const fq_status st = prepare_product<CG, SPLIT, FUSE>(sms, room)) return st;
   const int grid = SPLIT ? a.units * a.KS : std::min(a.units, room.fit[CG - 1]) * CG;
   return launch(mxfp_product_kernel<CG, SPLIT, FUSE>, dim3(static_cast<unsigned>(grid)), kThreads,
-                static_cast<size_t>(a.stages) * a.stage_bytes + a.x_bytes + kTailBytes + 1024,
+                static_cast<size_t>(a.stages) * a.stage_bytes + a.x_bytes + part_bytes(a) +
+                    kTailBytes + 1024,
                 SPLIT ? a.KS : CG, s, mw, mx, a) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
@@ -833,17 +839,17 @@ fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const Pro
 
 // The tiles of M tokens and W.  Of every width (all of up to 192 tokens, or tiles of 64, 128 or 192,
 // as scales of X have to start on an even column of their tile), by one CTA, a pair, or 2 to 8 CTAs
-// that split k where all of them fit at once, the one that takes the least time.  In ns, fitted to 4 to 43 stages of
-// 1024 to 28672 rows:
+// that split k where all of them fit at once, the one that takes the least time.  In ns, fitted to 4
+// to 43 stages of 1024 to 28672 rows:
 //   a stage 210 up to 128 tokens, 250 at 192; one of several rounds of tiles its stages, or 500 + 7
 //   a token if storing the tile before takes longer, and 15% more on single CTAs (their reads from
 //   L2: 4096 tokens, 28672 x 8192 260 us in pairs, 314 without); the last tile 7 a token; a split
-//   1500 + 8 a token for the exchange.
+//   1150 + 8 a token for the exchange.
 // Measured, with what a rule of all tokens to a tile and as many splits as fit took: 256 tokens,
-// 4096 x 4096 6.7 us (64 wide, no split) and 11.0; 128 tokens, 1024 x 4096 6.3 (64 wide, 4 splits)
-// and 7.6 (128 wide, 8); 192 tokens, 4096 x 1024 3.9 (64 wide) and 7.8 (192 wide, 2 splits).
-// A split pays at one token: 1024 x 11008 5.6 us with 8, 11.8 without; 4096 x 4096 5.4 with 4, 6.4;
-// 4096 x 1024 4.8 with 2, 3.7 without.
+// 4096 x 4096 6.6 us (64 wide, no split) and 11.0; 192 tokens, 4096 x 1024 3.9 (64 wide) and 7.8
+// (192 wide, 2 splits).  A split pays where k is long: one token, 1024 x 11008 5.3 us with 8, 11.9
+// without; 4096 x 4096 5.2 with 4, 6.4; 4096 x 1024 4.3 with 2, 3.6 without; 128 tokens, 1024 x
+// 4096 5.3 with 4, 6.5.
 void plan_tiles(ProdArgs& a, int& cg, int sms, const Room& pairs, const Room& splits) {
   const int most = a.M <= kBN ? static_cast<int>(round_up(a.M, 16)) : kBN;
   int64_t least = -1;
@@ -855,10 +861,10 @@ void plan_tiles(ProdArgs& a, int& cg, int sms, const Room& pairs, const Room& sp
       const int64_t rounds = ceil_div(units, c == 2 ? pairs.fit[1] : sms);
       const int64_t stage = 210 + std::max(0, bn - 128) * 5 / 8;
       for (int i = 0; i < (c == 1 ? 4 : 1); ++i) {
-        if (i && (units > splits.fit[i] || a.KB < 2 << i)) break;
+        if (i && (bn > kSplitTokens || units > splits.fit[i] || a.KB < 2 << i)) break;
         int64_t round = ceil_div(a.KB, 1 << i) * stage;
         if (rounds > 1) round = std::max<int64_t>(round, 500 + 7 * bn) * (c == 1 ? 115 : 100) / 100;
-        const int64_t time = rounds * round + 7 * bn + (i ? 1500 + 8 * bn : 0);
+        const int64_t time = rounds * round + 7 * bn + (i ? 1150 + 8 * bn : 0);
         if (least < 0 || time < least) {
           least = time;
           a.bn = bn;
@@ -895,7 +901,7 @@ fq_status product(const fq_mxfp& X, const fq_mxfp& W, void* y, int32_t* status, 
   ProdArgs a{};
   if (const fq_status st = plan_product(a, X.rows, W, sms, cg)) return st;
   a.stage_bytes = stage_bytes(a.bn / cg);
-  a.stages = stages_for(a.stage_bytes, 0);
+  a.stages = stages_for(a.stage_bytes, part_bytes(a));
   a.sx = X.scales;
   a.early_w = early_w;
   a.y = static_cast<__nv_bfloat16*>(y);
@@ -924,7 +930,7 @@ bool fused_product(const void* x, int M, const fq_mxfp& W, void* y, int32_t* sta
   }
   a.x_bytes = range * (kXBlock + kXScales);
   a.stage_bytes = kABytes;
-  a.stages = stages_for(a.stage_bytes, a.x_bytes);
+  a.stages = stages_for(a.stage_bytes, a.x_bytes + part_bytes(a));
   a.x = static_cast<const uint4*>(x);
   a.y = static_cast<__nv_bfloat16*>(y);
   a.status = status;
