@@ -720,8 +720,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   // before the TMEM goes and the pair parts.
   tc_fence_before_sync();
   __syncthreads();
-  __syncwarp();
-  if (CG == 2) cluster_sync();
+  if (CG == 2) {
+    __syncwarp();                                 // the pair's barrier takes whole warps
+    cluster_sync();
+  }
   if (warp == 1) {
     tc_fence_after_sync();
     tmem_dealloc_cg<CG>(tmem_base, kTmemCols);
@@ -1403,24 +1405,30 @@ size_t fq_head_grad_workspace_bytes(int M, int d, int V, int K) {
 fq_status fq_cross_entropy(const void* x, int M, int d, const void* W, int V,
                            const int32_t* target, float* loss, float* lse, void* ws,
                            size_t ws_bytes, fq_stream_t stream) {
-  return head_loss(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, loss, lse, ws, ws_bytes,
-                   reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    return head_loss(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, loss, lse, ws, ws_bytes,
+                     reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 fq_status fq_cross_entropy_grad(const void* x, int M, int d, const void* W, int V,
                                 const int32_t* target, const float* lse, const float* dloss,
                                 void* dx, void* dW, void* ws, size_t ws_bytes,
                                 fq_stream_t stream) {
-  return head_grad(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, lse, dloss, dx, dW, ws,
-                   ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    return head_grad(x, M, d, W, V, Target{target, nullptr, 1, 1.f}, lse, dloss, dx, dW, ws,
+                     ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 fq_status fq_distill(const void* x, int M, int d, const void* W, int V, const int32_t* index,
                      const float* logit, int K, float tau, float* loss, float* lse, void* ws,
                      size_t ws_bytes, fq_stream_t stream) {
   if (!logit) return FQ_ERR_INVALID_ARG;
-  return head_loss(x, M, d, W, V, Target{index, logit, K, tau}, loss, lse, ws, ws_bytes,
-                   reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    return head_loss(x, M, d, W, V, Target{index, logit, K, tau}, loss, lse, ws, ws_bytes,
+                     reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 fq_status fq_distill_grad(const void* x, int M, int d, const void* W, int V,
@@ -1428,8 +1436,10 @@ fq_status fq_distill_grad(const void* x, int M, int d, const void* W, int V,
                           const float* lse, const float* dloss, void* dx, void* dW, void* ws,
                           size_t ws_bytes, fq_stream_t stream) {
   if (!logit) return FQ_ERR_INVALID_ARG;
-  return head_grad(x, M, d, W, V, Target{index, logit, K, tau}, lse, dloss, dx, dW, ws, ws_bytes,
-                   reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    return head_grad(x, M, d, W, V, Target{index, logit, K, tau}, lse, dloss, dx, dW, ws, ws_bytes,
+                     reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 }  // extern "C"

@@ -35,6 +35,16 @@ constexpr int kWsMaxTiles = 640;
 static_assert(kWsFlags + 3 * kWsMaxTiles * kWsSlices * 4 <= kWsHeader, "flags fit the header");
 constexpr int kDecodeMaxM = 64;   // batches up to this size take the fused decode kernel
 
+// The body of a C entry: no exception (the host's memory or a lock ran out) leaves it.
+template <typename F>
+fq_status guarded(F&& body) noexcept {
+  try {
+    return body();
+  } catch (...) {
+    return FQ_ERR_CUDA;
+  }
+}
+
 // ---- fq_api.cu
 }  // namespace fq
 extern "C" size_t fq_packed_words(int n_out, int n_in);

@@ -978,25 +978,29 @@ fq_status fq_mxfp_quantize(const void* x, int rows, int cols, const fq_mxfp* q,
   if (const fq_status st = check_mxfp(q)) return st;
   if (q->rows != rows || q->cols != cols) return FQ_ERR_INVALID_ARG;
   if (!aligned16(x)) return FQ_ERR_ALIGNMENT;
-  int sms = 0;
-  if (const fq_status st = device_sms(sms)) return st;
-  return quantize(x, *q, reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    int sms = 0;
+    if (const fq_status st = device_sms(sms)) return st;
+    return quantize(x, *q, reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 fq_status fq_mxfp_dequantize(const fq_mxfp* q, void* y, fq_stream_t stream) {
   if (!y) return FQ_ERR_INVALID_ARG;
   if (const fq_status st = check_mxfp(q)) return st;
   if (!aligned16(y)) return FQ_ERR_ALIGNMENT;
-  int sms = 0;
-  if (const fq_status st = device_sms(sms)) return st;
-  const int KB = stages_of(q->cols);
-  return launch(mxfp_dequantize_kernel, q_grid(q->rows, KB), kQThreads, 0, 1,
-                reinterpret_cast<cudaStream_t>(stream),
-                reinterpret_cast<const uint32_t*>(q->codes),
-                static_cast<const uint8_t*>(q->scales), q->rows, q->cols, KB,
-                static_cast<uint4*>(y)) == cudaSuccess
-             ? FQ_OK
-             : FQ_ERR_CUDA;
+  return guarded([&] {
+    int sms = 0;
+    if (const fq_status st = device_sms(sms)) return st;
+    const int KB = stages_of(q->cols);
+    return launch(mxfp_dequantize_kernel, q_grid(q->rows, KB), kQThreads, 0, 1,
+                  reinterpret_cast<cudaStream_t>(stream),
+                  reinterpret_cast<const uint32_t*>(q->codes),
+                  static_cast<const uint8_t*>(q->scales), q->rows, q->cols, KB,
+                  static_cast<uint4*>(y)) == cudaSuccess
+               ? FQ_OK
+               : FQ_ERR_CUDA;
+  });
 }
 
 fq_status fq_mxfp_product(const fq_mxfp* X, const fq_mxfp* W, void* y, int32_t* status,
@@ -1006,9 +1010,11 @@ fq_status fq_mxfp_product(const fq_mxfp* X, const fq_mxfp* W, void* y, int32_t* 
   if (const fq_status st = check_mxfp(W)) return st;
   if (X->cols != W->cols) return FQ_ERR_INVALID_ARG;
   if (!aligned16(y) || (status && reinterpret_cast<uintptr_t>(status) % 4)) return FQ_ERR_ALIGNMENT;
-  int sms = 0;
-  if (const fq_status st = device_sms(sms)) return st;
-  return product(*X, *W, y, status, sms, false, reinterpret_cast<cudaStream_t>(stream));
+  return guarded([&] {
+    int sms = 0;
+    if (const fq_status st = device_sms(sms)) return st;
+    return product(*X, *W, y, status, sms, false, reinterpret_cast<cudaStream_t>(stream));
+  });
 }
 
 size_t fq_mxfp_workspace_bytes(int M, int d_in, int d_out) {
@@ -1025,17 +1031,19 @@ fq_status fq_mxfp_linear(const void* x, int M, int d_in, const fq_mxfp* W, void*
   if (!ws) return FQ_ERR_WORKSPACE;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return FQ_ERR_ALIGNMENT;
   if (ws_bytes < fq_mxfp_workspace_bytes(M, d_in, W->rows)) return FQ_ERR_WORKSPACE;
-  int sms = 0;
-  if (const fq_status st = device_sms(sms)) return st;
-  const Ws L = ws_layout(M, d_in);
-  auto* w = static_cast<uint8_t*>(ws);
-  const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
-  auto s = reinterpret_cast<cudaStream_t>(stream);
-  auto* status = static_cast<int32_t*>(ws);
-  fq_status st = FQ_OK;
-  if (fused_product(x, M, *W, y, status, sms, s, st)) return st;
-  if ((st = quantize(x, X, s)) != FQ_OK) return st;
-  return product(X, *W, y, status, sms, true, s);
+  return guarded([&] {
+    int sms = 0;
+    if (const fq_status st = device_sms(sms)) return st;
+    const Ws L = ws_layout(M, d_in);
+    auto* w = static_cast<uint8_t*>(ws);
+    const fq_mxfp X{w + L.codes, w + L.scales, M, d_in};
+    auto s = reinterpret_cast<cudaStream_t>(stream);
+    auto* status = static_cast<int32_t*>(ws);
+    fq_status st = FQ_OK;
+    if (fused_product(x, M, *W, y, status, sms, s, st)) return st;
+    if ((st = quantize(x, X, s)) != FQ_OK) return st;
+    return product(X, *W, y, status, sms, true, s);
+  });
 }
 
 }  // extern "C"
