@@ -291,7 +291,8 @@ def _stream(stream) -> int | None:
     if _current is None:
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        device = torch.cuda.current_device
+        torch.cuda.current_device()               # torch's CUDA state is up from here on
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _current = ((lambda: raw(device())) if raw is not None
                     else lambda: torch.cuda.current_stream().cuda_stream)
     return _current()

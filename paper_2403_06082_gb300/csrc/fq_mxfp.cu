@@ -25,11 +25,11 @@
 // tiles' traffic from L2 is what bounds a large product, and this cuts it by 28%.
 //
 // Few tokens read W once at memory speed; the tiles are then too few for the SMs, so a cluster of
-// KS CTAs splits the k range of one tile.  Each CTA finishes every KS-th token: all write their parts
-// of it to that CTA's shared memory, where they are added up in rank order.  (Parts kept at home and
-// read by their adder cost a second barrier: 64 tokens, 1024 x 4096 6.0 us, 4.7 this way; one token,
-// 4096 x 4096 5.4 and 5.2.)  The room for parts leaves five stages at 128 tokens, the most that a
-// split tile has.
+// KS CTAs splits the k range of one tile.  Each CTA finishes every KS-th token: all write their
+// parts of it to that CTA's shared memory, where they are added up in rank order.  (Parts kept at
+// home and read by their adder cost a second barrier: 64 tokens, 1024 x 4096 6.0 us, 4.7 this way;
+// one token, 4096 x 4096 5.4 and 5.2.)  The room for parts leaves five stages at 128 tokens, the
+// most that a split tile has.
 //
 // Up to 16 tokens the product takes bf16 x itself (FUSE): each CTA's epilogue warps quantise its k
 // range of x into shared memory, for all of its tiles, while W's first stages arrive.  One launch
@@ -768,7 +768,8 @@ dim3 q_grid(int rows, int KB) {
 
 fq_status quantize(const void* x, const fq_mxfp& q, cudaStream_t s) {
   const int KB = stages_of(q.cols);
-  return launch(mxfp_quantize_kernel, q_grid(q.rows, KB), kQThreads, 0, 1, s, static_cast<const uint4*>(x), q.rows, q.cols, KB,
+  return launch(mxfp_quantize_kernel, q_grid(q.rows, KB), kQThreads, 0, 1, s,
+                static_cast<const uint4*>(x), q.rows, q.cols, KB,
                 reinterpret_cast<uint32_t*>(q.codes), q.scales) == cudaSuccess
              ? FQ_OK
              : FQ_ERR_CUDA;
@@ -837,10 +838,10 @@ fq_status launch_product(const CUtensorMap& mw, const CUtensorMap& mx, const Pro
              : FQ_ERR_CUDA;
 }
 
-// The tiles of M tokens and W.  Of every width (all of up to 192 tokens, or tiles of 64, 128 or 192,
-// as scales of X have to start on an even column of their tile), by one CTA, a pair, or 2 to 8 CTAs
-// that split k where all of them fit at once, the one that takes the least time.  In ns, fitted to 4
-// to 43 stages of 1024 to 28672 rows:
+// The tiles of M tokens and W.  Of every width (all of up to 192 tokens, or tiles of 64, 128 or
+// 192, as scales of X have to start on an even column of their tile), by one CTA, a pair, or 2 to 8
+// CTAs that split k where all of them fit at once, the one that takes the least time.  In ns, fitted
+// to 4 to 43 stages of 1024 to 28672 rows:
 //   a stage 210 up to 128 tokens, 250 at 192; one of several rounds of tiles its stages, or 500 + 7
 //   a token if storing the tile before takes longer, and 15% more on single CTAs (their reads from
 //   L2: 4096 tokens, 28672 x 8192 260 us in pairs, 314 without); the last tile 7 a token; a split
